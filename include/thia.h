@@ -454,6 +454,59 @@ int thia_classifier_op_pool(thia_classifier* c, const void* in, int n, int H, in
 int thia_classifier_op_unit(thia_classifier* c, const void* feat, int n, int HW, int ep, int32_t* out_labels, float* out_conf,
                             float* out_logits);
 
+/* ---------------------------------------------------------------- rows in 8 bits
+ * Rows of 8-bit whole numbers with one scale each, what makes them, and the product of two such matrices: the wide layers of a
+ * box head (or any other matrix product over rows) on the 8-bit matrix instructions, with half the bytes of bf16.
+ *
+ * A row y of k values is held as codes q[j] in -127..127 and a scale s, standing for q[j] * s: s = max|y| / 127 and q[j] =
+ * y[j] / s rounded to nearest (ties to even).  A row of zeros has scale 0 and codes 0; a row with a NaN or an infinity has
+ * scale NaN and codes 0, so that whatever is computed from it is NaN.  Codes lie in rows of thia_i8_pitch(k) bytes (k
+ * rounded up to whole lines of 128), codes dev int8 [rows, pitch] and 16-byte aligned; the bytes behind column k are written as
+ * zeros and never matter when read.  k is 1..65536.
+ *
+ * These calls belong to no model: they take the stream (hip_stream as in thia_set_stream) as an argument, run on the current HIP
+ * device, allocate nothing, share nothing between calls and never wait (the loading calls excepted), so they may be captured
+ * into graphs and called from several threads.  precision: 0 = float32, 1 = bf16 elements.  Row pitches ld* count elements and may
+ * exceed the row; rows need only their element's alignment.  rows = 0 does nothing.  Errors as for the other calls, the
+ * message per thread from thia_i8_last_error().
+ */
+const char* thia_i8_last_error(void);
+
+/* Bytes from one row of codes to the next; 0 if k is not within 1..65536. */
+int thia_i8_pitch(int k);
+
+/* Rows x dev T [rows, k] (pitch ldx) -> codes, scales dev float32 [rows]. */
+int thia_quantize_rows(const void* x, long long ldx, int precision, int rows, int k, int8_t* codes, float* scales,
+                       void* hip_stream);
+
+/* The residual's addition and a root-mean-square norm in front of an 8-bit product, in one pass: h = x + residual in fp32,
+ * sum = h rounded to T, y[j] = h[j] gain[j] / sqrt(mean(h^2) + eps), y's codes and scales as above.  x, residual (NULL: h = x) and
+ * sum (NULL: not wanted; needs a residual) dev T [rows, k] with pitches ldx, ldr, ldsum; sum may be x or residual itself (same pitch), and
+ * must not overlap them otherwise.  gain dev float32 [k].  eps > 0. */
+int thia_rms_norm_i8(const void* x, long long ldx, const void* residual, long long ldr, const float* gain, float eps,
+                     int precision, int rows, int k, void* sum, long long ldsum, int8_t* codes, float* scales,
+                     void* hip_stream);
+
+/* One layer's weights, resident in 8 bits on the device that is current at the call: n channels (1..2^20) of k values.  Either from
+ * fp32 weights [n, k], each channel quantized as thia_quantize_rows does, or from given codes [n, k] (dense; -128 is
+ * allowed) and scales [n].  bias [n] or NULL.  All may be host or device memory; device memory must hold its values already.
+ * Blocking (allocates, uploads and lays the weights out); the arguments may be freed after the call. */
+typedef struct thia_linear_i8 thia_linear_i8;
+int thia_linear_i8_load(const float* weights, const float* bias, int n, int k, thia_linear_i8** out);
+int thia_linear_i8_load_codes(const int8_t* codes, const float* scales, const float* bias, int n, int k,
+                              thia_linear_i8** out);
+/* Frees the weights; waits for the device.  NULL is allowed. */
+void thia_linear_i8_free(thia_linear_i8* l);
+int thia_linear_i8_shape(const thia_linear_i8* l, int* n, int* k);
+
+/* out[m, c] = act(scales[m] wscale[c] sum_j codes[m, j] wcodes[c, j] + bias[c] + residual[m, c]): the sum exact in 32-bit whole
+ * numbers, the rest in fp32, one rounding to T.  codes, scales as above ([rows, thia_i8_pitch(k)], [rows]; -128 is allowed), residual
+ * dev T [rows, n] (pitch ldr) or NULL, relu 0 or 1 (a NaN stays), out dev T [rows, n] (pitch ldo), T per precision.  out may be
+ * residual itself (same pitch) and must not overlap any input otherwise.  A row's result does not depend on the other rows or on
+ * their number.  The layer's device must be the current one. */
+int thia_linear_i8_run(const thia_linear_i8* l, const int8_t* codes, const float* scales, int rows, const void* residual,
+                       long long ldr, int relu, int precision, void* out, long long ldo, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

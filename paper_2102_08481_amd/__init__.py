@@ -4,6 +4,7 @@
 The names below mirror the C entry points; they only marshal arguments.
 """
 from .binding import (Model, Classifier, ThiaError, ThiaInfo, ThiaQuery, ThiaPlannerCfg, ThiaPlanStats, lib, planner_cfg, plan_from_flags, metrics_from_counts,
+                      LinearI8, quantize_rows, rms_norm_i8,
                       EXPORTS, TAPS, KERNEL_CLASSES, LIB_PATH)
 
 
@@ -59,3 +60,28 @@ def thia_classifier_load(weights, n_exits, device="cuda:0"):
 def thia_classify_chunk(classifier, frames, ep, want_logits=False):
     """frames: cuda uint8 [n,3,H,W]; ep in 1..n_exits or 0 (skip).  Returns (labels, confidence[, logits])."""
     return classifier.classify_chunk(frames, ep, want_logits)
+
+
+def thia_quantize_rows(x, out=None):
+    """x: cuda float32 / bfloat16 [rows, k].  Returns (codes int8 [rows, pitch], scales float32 [rows])."""
+    return quantize_rows(x, out)
+
+
+def thia_rms_norm_i8(x, gain, eps=1e-6, residual=None, sum_out=None, out=None):
+    """Root-mean-square norm of x + residual in 8 bits.  Returns (codes, scales, sum or None)."""
+    return rms_norm_i8(x, gain, eps, residual, sum_out, out)
+
+
+def thia_linear_i8_load(weights, bias=None, device=None):
+    """weights: float32 [n, k], quantized per channel.  Returns the resident 8-bit layer."""
+    return LinearI8(weights, bias, None, device)
+
+
+def thia_linear_i8_load_codes(codes, scales, bias=None, device=None):
+    """codes: int8 [n, k], scales: float32 [n].  Returns the resident 8-bit layer."""
+    return LinearI8(codes, bias, scales, device)
+
+
+def thia_linear_i8_run(layer, codes, scales, relu=False, residual=None, out_f32=False, out=None):
+    """codes int8 [rows, pitch], scales float32 [rows] -> [rows, n], bfloat16 or float32."""
+    return layer.run(codes, scales, relu, residual, out_f32, out)

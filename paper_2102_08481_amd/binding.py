@@ -30,7 +30,9 @@ EXPORTS = ["thia_load_model", "thia_free_model", "thia_set_stream", "thia_set_mi
            "thia_op_rpn_proposals", "thia_op_nms", "thia_op_nms_noalloc", "thia_op_roialign", "thia_op_select_detections", "thia_op_conv",
            "thia_op_stem", "thia_op_bottleneck", "thia_op_bottleneck_tail", "thia_set_fusion", "thia_set_lanes",
            "thia_classifier_load", "thia_classifier_free", "thia_classifier_set_stream", "thia_classifier_last_error",
-           "thia_classify_chunk", "thia_classifier_op_pool", "thia_classifier_op_unit"]
+           "thia_classify_chunk", "thia_classifier_op_pool", "thia_classifier_op_unit",
+           "thia_i8_last_error", "thia_i8_pitch", "thia_quantize_rows", "thia_rms_norm_i8", "thia_linear_i8_load",
+           "thia_linear_i8_load_codes", "thia_linear_i8_free", "thia_linear_i8_shape", "thia_linear_i8_run"]
 
 
 class ThiaInfo(C.Structure):
@@ -125,6 +127,18 @@ def lib():
     L.thia_classify_chunk.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, vp]
     L.thia_classifier_op_pool.argtypes = [vp, vp, i32, i32, i32, i32, vp]
     L.thia_classifier_op_unit.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp]
+    i64 = C.c_longlong
+    L.thia_i8_last_error.argtypes = []
+    L.thia_i8_last_error.restype = C.c_char_p
+    L.thia_i8_pitch.argtypes = [i32]
+    L.thia_quantize_rows.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp]
+    L.thia_rms_norm_i8.argtypes = [vp, i64, vp, i64, vp, C.c_float, i32, i32, i32, vp, i64, vp, vp, vp]
+    L.thia_linear_i8_load.argtypes = [vp, vp, i32, i32, C.POINTER(vp)]
+    L.thia_linear_i8_load_codes.argtypes = [vp, vp, vp, i32, i32, C.POINTER(vp)]
+    L.thia_linear_i8_free.argtypes = [vp]
+    L.thia_linear_i8_free.restype = None
+    L.thia_linear_i8_shape.argtypes = [vp, vp, vp]
+    L.thia_linear_i8_run.argtypes = [vp, vp, vp, i32, vp, i64, i32, i32, vp, i64, vp]
     for name in EXPORTS:
         getattr(L, name)
     _lib = L
@@ -529,6 +543,153 @@ class Classifier:
     def close(self):
         if self._h:
             lib().thia_classifier_free(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ---------------------------------------------------------------- rows in 8 bits
+_I8_TYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _i8_check(rc):
+    if rc:
+        raise ThiaError(rc, lib().thia_i8_last_error().decode())
+
+
+def _i8_rows(name, t, dtype, device, shape):
+    """Tensor argument as (pointer, row pitch): [rows, k] with dense rows, any pitch; None passes."""
+    if t is None:
+        return None, 0
+    if t.device != device or t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {dtype} {list(shape)} on {device}, not {t.dtype} {list(t.shape)} on {t.device}")
+    rows, k = shape
+    if (k > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < k):
+        raise ValueError(f"{name}: the values of a row must lie side by side and rows must not overlap")
+    return t.data_ptr(), t.stride(0) if rows > 1 else k
+
+
+def _i8_vector(name, t, n, device):
+    if t.device != device or t.dtype != torch.float32 or tuple(t.shape) != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a dense float32 [{n}] on {device}")
+    return t.data_ptr()
+
+
+def _i8_input(x):
+    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == 2 and x.dtype in _I8_TYPES):
+        raise ValueError("rows must be a two-dimensional float32 or bfloat16 tensor on the GPU")
+    return x.shape[0], x.shape[1], x.device
+
+
+def _i8_codes(rows, k, device, out):
+    """Codes and scales to write, new or given, as (codes, scales)."""
+    pitch = lib().thia_i8_pitch(k)
+    if not pitch:
+        raise ThiaError(-3, "rows of codes hold 1 to 65536 values")
+    if out is None:
+        return torch.empty((rows, pitch), dtype=torch.int8, device=device), torch.empty(rows, dtype=torch.float32, device=device)
+    codes, scales = out
+    _i8_given(codes, scales, rows, pitch, device)
+    return codes, scales
+
+
+def _i8_given(codes, scales, rows, pitch, device):
+    if codes.device != device or codes.dtype != torch.int8 or tuple(codes.shape) != (rows, pitch) or not codes.is_contiguous():
+        raise ValueError(f"codes must be dense int8 [{rows}, {pitch}] on {device}")
+    _i8_vector("scales", scales, rows, device)
+
+
+def _stream(device):
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def quantize_rows(x, out=None):
+    """x: float32 / bfloat16 cuda [rows, k] (dense rows, any pitch) -> (codes int8 [rows, pitch], scales float32 [rows]), on torch's
+    current stream; out: such a pair to write into."""
+    rows, k, device = _i8_input(x)
+    xp, ldx = _i8_rows("x", x, x.dtype, device, (rows, k))
+    codes, scales = _i8_codes(rows, k, device, out)
+    with torch.cuda.device(device):
+        _i8_check(lib().thia_quantize_rows(xp, ldx, _I8_TYPES[x.dtype], rows, k, codes.data_ptr(), scales.data_ptr(), _stream(device)))
+    return codes, scales
+
+
+def rms_norm_i8(x, gain, eps=1e-6, residual=None, sum_out=None, out=None):
+    """Norm of x + residual in 8 bits: (codes, scales, sum), sum = x + residual in x's type (None without a residual).  sum_out: where
+    it goes (may be x or residual); out: (codes, scales) to write into."""
+    rows, k, device = _i8_input(x)
+    xp, ldx = _i8_rows("x", x, x.dtype, device, (rows, k))
+    rp, ldr = _i8_rows("residual", residual, x.dtype, device, (rows, k))
+    gp = _i8_vector("gain", gain, k, device)
+    if residual is None and sum_out is not None:
+        raise ValueError("a sum without a residual")
+    if residual is not None and sum_out is None:
+        sum_out = torch.empty((rows, k), dtype=x.dtype, device=device)
+    sp, lds = _i8_rows("sum_out", sum_out, x.dtype, device, (rows, k))
+    codes, scales = _i8_codes(rows, k, device, out)
+    with torch.cuda.device(device):
+        _i8_check(lib().thia_rms_norm_i8(xp, ldx, rp, ldr, gp, eps, _I8_TYPES[x.dtype], rows, k, sp, lds, codes.data_ptr(), scales.data_ptr(),
+                                         _stream(device)))
+    return codes, scales, sum_out
+
+
+class LinearI8:
+    """One layer's weights, resident in 8 bits (thia_linear_i8*).  weights: float32 [n, k], or with `scales` (float32 [n]) int8 codes
+    [n, k]; bias float32 [n] or None; numpy arrays or tensors, on the host or on `device`."""
+
+    def __init__(self, weights, bias=None, scales=None, device=None):
+        self._h = None
+        if device is None:
+            device = weights.device if isinstance(weights, torch.Tensor) and weights.is_cuda else "cuda:0"
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        given = [None if v is None else torch.as_tensor(v).detach().to(t).contiguous()
+                 for v, t in ((weights, torch.float32 if scales is None else torch.int8), (scales, torch.float32), (bias, torch.float32))]
+        w, s, b = given
+        if w.dim() != 2 or any(v is not None and tuple(v.shape) != (w.shape[0],) for v in (s, b)):
+            raise ValueError("weights must be [n, k], scales and bias [n]")
+        if scales is not None and torch.as_tensor(weights).dtype != torch.int8:
+            raise ValueError("codes must be int8")
+        if any(v is not None and v.is_cuda and v.device != self.device for v in given):
+            raise ValueError(f"weights must lie on the host or on {self.device}")
+        self.n, self.k = w.shape
+        self.pitch = lib().thia_i8_pitch(self.k)
+        h, ptr = C.c_void_p(), lambda v: None if v is None else v.data_ptr()
+        with torch.cuda.device(self.device):
+            torch.zeros(1, device=self.device)          # make sure the HIP context exists
+            torch.cuda.current_stream().synchronize()   # the library reads the weights outside torch's stream
+            if scales is None:
+                rc = lib().thia_linear_i8_load(ptr(w), ptr(b), self.n, self.k, C.byref(h))
+            else:
+                rc = lib().thia_linear_i8_load_codes(ptr(w), ptr(s), ptr(b), self.n, self.k, C.byref(h))
+        _i8_check(rc)
+        self._h = h
+
+    def run(self, codes, scales, relu=False, residual=None, out_f32=False, out=None):
+        """codes int8 [rows, pitch], scales float32 [rows] -> [rows, n] in bfloat16 (float32 with out_f32), on torch's current stream.
+        residual: [rows, n] of that type, added in front of the ReLU; out: where the result goes (may be residual)."""
+        if self._h is None:
+            raise ThiaError(-1, "the layer has been freed")
+        rows, dtype = scales.shape[0] if scales.dim() == 1 else -1, torch.float32 if out_f32 else torch.bfloat16
+        _i8_given(codes, scales, rows, self.pitch, self.device)
+        if out is None:
+            out = torch.empty((rows, self.n), dtype=dtype, device=self.device)
+        rp, ldr = _i8_rows("residual", residual, dtype, self.device, (rows, self.n))
+        op, ldo = _i8_rows("out", out, dtype, self.device, (rows, self.n))
+        with torch.cuda.device(self.device):
+            _i8_check(lib().thia_linear_i8_run(self._h, codes.data_ptr(), scales.data_ptr(), rows, rp, ldr, int(relu), int(not out_f32), op,
+                                               ldo, _stream(self.device)))
+        return out
+
+    def close(self):
+        if self._h:
+            with torch.cuda.device(self.device):
+                lib().thia_linear_i8_free(self._h)
             self._h = None
 
     def __del__(self):

@@ -212,6 +212,12 @@ hipError_t launch_select(const float* scores, const float* boxes, const int32_t*
 // fills the empty pattern for n frames
 hipError_t launch_fill_empty(int n, int D, float* out_boxes, float* out_scores, int32_t* out_labels, hipStream_t s);
 
+// ---------------------------------------------------------------- rows in 8 bits
+// Columns of a row of codes (a sum of so many products of two 8-bit numbers fits 32 bits) and channels of an 8-bit layer.
+constexpr int kMaxI8Cols = 65536, kMaxI8Channels = 1 << 20;
+// Keeps `why` (a string that lives on) as this thread's thia_i8_last_error and returns `code`.
+int i8_fail(int code, const char* why);
+
 // ---------------------------------------------------------------- query planning (host logic + the predicate kernel)
 // flags[r] = (number of slots d of row r with labels[r][d] == label and scores[r][d] >= min_score) >= min_count
 hipError_t launch_count_predicate(const int32_t* labels, const float* scores, long rows, int D, int label, int min_count,

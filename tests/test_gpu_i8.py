@@ -1,0 +1,342 @@
+"""Rows in 8 bits on the GPU, against their definition in 64 bits.
+
+Tolerances count roundings (u = 2^-24 is half a step of fp32, relative; 2^-8 of bf16):
+ - a scale max / 127: the quotient's and the store's, 2 u; with the norm the fp32 sum of squares as well: every square and every
+   addition that a value passes through (at most 64 in a thread's own sum and 16 across the block) 1 u, halved by the root, and the
+   root, the quotients and the gain's product: under 64 u.
+ - a code is y / s rounded, y / s formed from at most four rounded operations on values up to 127: off by at most half a step
+   and 127 * 4 u.
+ - a product: the whole sum to fp32, two factors, bias and residual: 5 u of the sum of their magnitudes, and the result's type."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: U}
+BF, F = torch.bfloat16, torch.float32
+
+
+def rows_of(seed, rows, k, dtype):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    x = torch.randn((rows, k), generator=g, device="cuda")
+    return (x * torch.exp(2 * torch.randn((rows, 1), generator=g, device="cuda"))).to(dtype)
+
+
+def check_codes(codes, scales, y, k, units):
+    """codes and scales of the rows y (64 bits, finite)."""
+    s = y.abs().amax(1) / 127
+    assert codes.shape == (y.shape[0], -(-k // 128) * 128) and (codes[:, k:] == 0).all()
+    assert ((scales.double() - s).abs() <= s * units * U + 2.0 ** -149).all()
+    q = codes[:, :k].double()
+    t = y / torch.where(s > 0, s, torch.ones_like(s))[:, None]
+    assert q.abs().max() <= 127 and ((q - t).abs() <= 0.5 + 127 * 4 * U).all()
+
+
+QUANTIZE = [(1, 1), (3, 1), (1, 7), (5, 64), (2, 127), (130, 128), (7, 129), (33, 500), (3, 511), (4, 512), (3, 513), (257, 1024), (9, 1025), (5, 2047),
+            (300, 12544), (2, 8191), (2, 8193), (3, 16385), (1, 32769), (2, 65535), (1, 65536), (20000, 24), (9600, 1024)]
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("rows,k", QUANTIZE)
+def test_quantize(rows, k, dtype):
+    import paper_2102_08481_amd as thia
+    x = rows_of(rows + k, rows, k, dtype)
+    check_codes(*thia.thia_quantize_rows(x), x.double(), k, 2)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("rows,k", QUANTIZE)
+def test_norm(rows, k, residual, dtype):
+    import paper_2102_08481_amd as thia
+    x, r = rows_of(rows + k, rows, k, dtype), rows_of(rows + k + 1, rows, k, dtype) if residual else None
+    gain, eps = 0.5 + torch.rand(k, device="cuda"), 1e-3
+    codes, scales, total = thia.thia_rms_norm_i8(x, gain, eps, r)
+    h = x.double() + (r.double() if residual else 0)
+    assert (total is None) == (not residual)
+    if residual:
+        assert torch.equal(total, (x.float() + r.float()).to(dtype))
+        h = (x.float() + r.float()).double()   # the sum is held in fp32
+    check_codes(codes, scales, h * gain.double() / torch.sqrt((h * h).mean(1, keepdim=True) + eps), k, 64)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("k", [5, 1000, 9000, 40000])
+def test_rows_without_values_and_extreme_rows(k, dtype):
+    """Rows of zeros, of the smallest and of the largest values, and rows with NaN or infinity among ordinary ones."""
+    import paper_2102_08481_amd as thia
+    x = rows_of(k, 12, k, dtype)
+    x[1], x[3] = 0, 0
+    x[3, k // 2] = 2.0 ** -133            # a single value, below the normal numbers
+    x[4] = x[4].sign() * 3.0e38
+    x[5] = x[5].sign() * 1.0e-38
+    x[6] = x[6].sign() * 2.0e25           # squares beyond fp32
+    x[7, k - 1], x[8, 0], x[9, k // 3] = float("nan"), float("inf"), -float("inf")
+    x[10] = -0.0
+    fine = torch.tensor([0, 1, 2, 3, 4, 5, 6, 10, 11], device="cuda")
+    gain = 0.5 + torch.rand(k, device="cuda")
+    for codes, scales, y, units in (
+            thia.thia_quantize_rows(x) + (x.double(), 2),
+            thia.thia_rms_norm_i8(x, gain, 1e-12)[:2] + (x.double() * gain.double() / torch.sqrt((x.double() ** 2).mean(1, keepdim=True) + 1e-12), 64)):
+        check_codes(codes[fine], scales[fine], y[fine], k, units)
+        assert scales[7:10].isnan().all() and (codes[7:10] == 0).all()
+        assert scales[1] == 0 and scales[10] == 0
+
+
+def test_norm_with_a_sum_that_overflows_or_cancels():
+    import paper_2102_08481_amd as thia
+    x = rows_of(1, 3, 777, F)
+    r = rows_of(2, 3, 777, F)
+    x[0, 3] = r[0, 3] = 3e38              # infinite as a sum
+    r[1] = -x[1]                          # nothing left
+    gain = torch.ones(777, device="cuda")
+    codes, scales, total = thia.thia_rms_norm_i8(x, gain, 1e-6, r)
+    assert torch.equal(total, x + r) and scales[0].isnan() and (codes[0] == 0).all() and scales[1] == 0 and (codes[1] == 0).all()
+    h = (x + r)[2:].double()
+    check_codes(codes[2:], scales[2:], h / torch.sqrt((h * h).mean(1, keepdim=True) + 1e-6), 777, 64)
+
+
+def test_norm_with_zero_and_large_gains():
+    import paper_2102_08481_amd as thia
+    x = rows_of(5, 4, 300, F)
+    for gain in (torch.zeros(300, device="cuda"), torch.full((300,), -1e-30, device="cuda"), torch.full((300,), 1e30, device="cuda")):
+        codes, scales, _ = thia.thia_rms_norm_i8(x * 1e-3, gain, 1e-6)
+        h = (x * 1e-3).double()
+        check_codes(codes, scales, h * gain.double() / torch.sqrt((h * h).mean(1, keepdim=True) + 1e-6), 300, 64)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("k", [37, 1000, 4099])
+def test_rows_with_pitches_on_odd_addresses_and_sums_in_place(k, dtype):
+    import paper_2102_08481_amd as thia
+    wide = rows_of(k, 19, 2 * k + 9, dtype)
+    x, r = wide[:, 1:k + 1], wide[:, k + 3:2 * k + 3]
+    gain = 0.5 + torch.rand(2 * k, device="cuda")[1:k + 1]
+    want = thia.thia_rms_norm_i8(x.contiguous(), gain, 1e-6, r.contiguous())
+    plain = thia.thia_quantize_rows(x.contiguous())
+    assert all(torch.equal(a, b) for a, b in zip(thia.thia_quantize_rows(x), plain))
+    room = torch.full((19, k + 5), 7, dtype=dtype, device="cuda")
+    got = thia.thia_rms_norm_i8(x, gain, 1e-6, r, sum_out=room[:, 2:k + 2])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert (room[:, :2] == 7).all() and (room[:, k + 2:] == 7).all()
+    for target in (0, 1):   # the sum in place of either input
+        again = wide.clone()
+        x, r = again[:, 1:k + 1], again[:, k + 3:2 * k + 3]
+        got = thia.thia_rms_norm_i8(x, gain, 1e-6, r, sum_out=(x, r)[target])
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        kept = torch.ones_like(wide, dtype=torch.bool)
+        kept[:, (1, k + 3)[target]:(k + 1, 2 * k + 3)[target]] = False
+        assert torch.equal(again[kept], wide[kept])
+
+
+def test_rows_behind_the_last_stay():
+    import paper_2102_08481_amd as thia
+    x = rows_of(3, 9, 200, BF)
+    codes, scales = torch.full((12, 256), 5, dtype=torch.int8, device="cuda"), torch.full((12,), 5.0, device="cuda")
+    thia.thia_quantize_rows(x, out=(codes[:9], scales[:9]))
+    assert (codes[9:] == 5).all() and (scales[9:] == 5).all()
+    want = thia.thia_quantize_rows(x)
+    assert torch.equal(codes[:9], want[0]) and torch.equal(scales[:9], want[1])
+
+
+# ---------------------------------------------------------------- the product
+def layer_of(seed, n, k, low=-127):
+    import paper_2102_08481_amd as thia
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    codes = torch.randint(low, 128, (n, k), generator=g, device="cuda", dtype=torch.int8)
+    scales, bias = 0.01 + torch.rand(n, generator=g, device="cuda"), torch.randn(n, generator=g, device="cuda") * 1000
+    return thia.thia_linear_i8_load_codes(codes, scales, bias), codes, scales, bias
+
+
+def codes_of(seed, rows, k, low=-127):
+    """Codes with anything behind column k."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    codes = torch.randint(low, 128, (rows, -(-k // 128) * 128), generator=g, device="cuda", dtype=torch.int8)
+    return codes, 0.01 + torch.rand(rows, generator=g, device="cuda")
+
+
+def check_product(out, codes, scales, w, ws, bias, k, relu=False, residual=None):
+    acc = torch.matmul(codes[:, :k].double(), w.double().t().contiguous())   # whole numbers below 2^53: exact
+    part = acc * scales.double()[:, None] * ws.double()
+    want, size = part + bias.double(), part.abs() + bias.double().abs()
+    if residual is not None:
+        want, size = want + residual.double(), size + residual.double().abs()
+    if relu:
+        want = want.clamp(min=0)
+    off = (out.double() - want).abs()
+    assert (off <= size * 5 * U * 1.001 + want.abs() * HALF[out.dtype] * 1.001).all(), float((off / size).max())
+
+
+LINEAR = [(1, 1, 1), (1, 16, 64), (2, 130, 3), (1, 4096, 4096), (3, 4097, 100), (15, 1000, 33), (16, 1024, 1024), (17, 512, 96), (31, 65, 31), (32, 64, 32),
+          (33, 128, 257), (63, 2000, 65), (64, 256, 64), (65, 300, 128), (100, 12544, 40), (127, 640, 129), (128, 128, 128), (300, 12544, 1024), (301, 384, 1000),
+          (1000, 700, 8), (1021, 1024, 250), (2000, 1024, 100), (2048, 256, 2048), (4096, 1024, 512), (5000, 513, 511), (1, 65536, 8), (40, 65536, 40),
+          (9600, 1024, 1024), (3000, 896, 2300), (20000, 64, 64), (70000, 16, 24), (2, 8, 300000)]
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("rows,k,n", LINEAR)
+def test_linear(rows, k, n, dtype):
+    import paper_2102_08481_amd as thia
+    layer, w, ws, b = layer_of(rows + n, n, k)
+    codes, scales = codes_of(k, rows, k)
+    out = thia.thia_linear_i8_run(layer, codes, scales, out_f32=dtype is F)
+    assert out.dtype == dtype and tuple(out.shape) == (rows, n)
+    check_product(out, codes, scales, w, ws, b, k)
+    residual = rows_of(7, rows, n, dtype) * 1000
+    check_product(thia.thia_linear_i8_run(layer, codes, scales, True, residual, dtype is F), codes, scales, w, ws, b, k, True, residual)
+
+
+@pytest.mark.parametrize("rows", [1, 20, 700, 4000])
+def test_the_largest_sums(rows):
+    """65536 products of -128 and -128: 2^30; and the layer takes -128 on both sides."""
+    import paper_2102_08481_amd as thia
+    k, n = 65536, 40
+    w = torch.full((n, k), -128, dtype=torch.int8, device="cuda")
+    w[1] = 127
+    layer = thia.thia_linear_i8_load_codes(w, torch.ones(n, device="cuda"))
+    out = thia.thia_linear_i8_run(layer, torch.full((rows, k), -128, dtype=torch.int8, device="cuda"), torch.ones(rows, device="cuda"), out_f32=True)
+    assert (out[:, 1] == -128.0 * 127 * k).all() and (out[:, 2:] == 2.0 ** 30).all() and (out[:, 0] == 2.0 ** 30).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_linear_with_pitches_in_place_and_beside(dtype):
+    import paper_2102_08481_amd as thia
+    for rows, k, n in ((5, 200, 37), (90, 200, 37), (700, 640, 130), (3000, 384, 515), (4000, 384, 512)):
+        layer, w, ws, b = layer_of(n, n, k)
+        codes, scales = codes_of(k, rows, k)
+        room = torch.full((rows + 2, n + 7), 7, dtype=dtype, device="cuda")
+        res = rows_of(9, rows, n + 3, dtype)[:, 1:n + 1]
+        want = thia.thia_linear_i8_run(layer, codes, scales, False, res.contiguous(), dtype is F)
+        thia.thia_linear_i8_run(layer, codes, scales, False, res, dtype is F, out=room[:rows, 3:n + 3])
+        assert torch.equal(room[:rows, 3:n + 3], want)
+        room[:rows, 3:n + 3] = 7
+        assert (room == 7).all()   # nothing beside the rows, and nothing behind the last
+        inplace = res.contiguous()
+        thia.thia_linear_i8_run(layer, codes, scales, False, inplace, dtype is F, out=inplace)
+        assert torch.equal(inplace, want)
+
+
+def test_a_row_does_not_depend_on_the_others():
+    import paper_2102_08481_amd as thia
+    layer, *_ = layer_of(1, 640, 896)
+    codes, scales = codes_of(2, 5000, 896)
+    every = thia.thia_linear_i8_run(layer, codes, scales)
+    for at, rows in ((0, 1), (17, 3), (100, 31), (500, 64), (700, 129), (1000, 300), (2000, 1000), (0, 4999)):
+        assert torch.equal(thia.thia_linear_i8_run(layer, codes[at:at + rows], scales[at:at + rows]), every[at:at + rows])
+
+
+@pytest.mark.parametrize("rows", [1, 50, 4000])
+def test_rows_that_are_not_numbers_stay_so_and_alone(rows):
+    import paper_2102_08481_amd as thia
+    layer, *_ = layer_of(1, 300, 256)
+    x = rows_of(4, rows, 256, BF)
+    x[rows // 2, 9] = float("nan")
+    codes, scales = thia.thia_quantize_rows(x)
+    for relu in (False, True):
+        out = thia.thia_linear_i8_run(layer, codes, scales, relu)
+        bad = torch.arange(rows, device="cuda") == rows // 2
+        assert out[bad].isnan().all() and not out[~bad].isnan().any()
+
+
+def test_layers_from_weights_and_without_rows():
+    import paper_2102_08481_amd as thia
+    w = rows_of(1, 45, 333, F)
+    q, s = thia.thia_quantize_rows(w)
+    bias = torch.randn(45)
+    codes, scales = codes_of(2, 70, 333)
+    want = thia.thia_linear_i8_run(thia.thia_linear_i8_load_codes(q[:, :333], s, bias.cuda()), codes, scales)
+    for weights, b in ((w, bias.cuda()), (w.cpu(), bias), (w.cpu().numpy(), bias.numpy()), (w, bias)):
+        layer = thia.thia_linear_i8_load(weights, b)
+        assert torch.equal(thia.thia_linear_i8_run(layer, codes, scales), want)
+    assert thia.thia_linear_i8_run(layer, codes[:0], scales[:0]).shape == (0, 45)
+    assert thia.thia_quantize_rows(w[:0])[0].shape == (0, 384)
+    assert thia.thia_rms_norm_i8(w[:0], torch.ones(333, device="cuda"))[1].shape == (0,)
+    plain = thia.thia_linear_i8_run(thia.thia_linear_i8_load(w), codes, scales, out_f32=True)
+    check_product(plain, codes, scales, q[:, :333], s, torch.zeros(45, device="cuda"), 333)
+    layer.close()
+    with pytest.raises(thia.ThiaError):
+        layer.run(codes, scales)
+
+
+def test_refusals_on_the_device():
+    import paper_2102_08481_amd as thia
+    layer, *_ = layer_of(1, 40, 200)
+    codes, scales = codes_of(2, 10, 200)
+    x = rows_of(1, 10, 200, BF)
+    one, cpu = torch.ones(200, device="cuda"), torch.zeros(10, 40, dtype=BF)
+    for call in (lambda: layer.run(codes[:, :200], scales), lambda: layer.run(codes, scales[:9]), lambda: layer.run(codes.float(), scales), lambda: layer.run(codes.cpu(), scales),
+                 lambda: layer.run(codes, scales.double()), lambda: layer.run(codes, scales, residual=cpu), lambda: layer.run(codes, scales, residual=cpu.cuda().float()),
+                 lambda: layer.run(codes, scales, residual=cpu.cuda(), out_f32=True), lambda: layer.run(codes, scales, out=cpu.cuda().t().contiguous().t()),
+                 lambda: layer.run(codes, scales, out=cpu.cuda()[:1].expand(10, 40)), lambda: thia.thia_quantize_rows(x.half()), lambda: thia.thia_quantize_rows(x.t()),
+                 lambda: thia.thia_quantize_rows(x[0]), lambda: thia.thia_rms_norm_i8(x, one[:199]), lambda: thia.thia_rms_norm_i8(x, one.double()),
+                 lambda: thia.thia_rms_norm_i8(x, one, residual=x.float()), lambda: thia.thia_rms_norm_i8(x, one, sum_out=x), lambda: thia.thia_rms_norm_i8(x, one, residual=x[:9])):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: thia.thia_rms_norm_i8(x, one, 0.0), lambda: thia.thia_quantize_rows(torch.zeros(1, 65537, device="cuda")),
+                 lambda: thia.thia_linear_i8_load(torch.zeros(1, 65537)), lambda: thia.thia_quantize_rows(x, out=(torch.empty(10 * 256 + 8, dtype=torch.int8, device="cuda")[8:].view(10, 256), scales))):
+        with pytest.raises(thia.ThiaError):
+            call()
+
+
+# ---------------------------------------------------------------- together
+def block(x, r, gain, up, down):
+    import paper_2102_08481_amd as thia
+    codes, scales, total = thia.thia_rms_norm_i8(x, gain, 1e-6, r)
+    u = thia.thia_linear_i8_run(up, codes, scales, relu=True)
+    c2, s2 = thia.thia_quantize_rows(u)
+    return codes, scales, total, u, c2, s2, thia.thia_linear_i8_run(down, c2, s2, residual=total)
+
+
+def block_parts(rows, k, n):
+    import paper_2102_08481_amd as thia
+    w1, w2 = rows_of(1, n, k, F) / k, rows_of(2, k, n, F) / n
+    b1, b2 = torch.randn(n, device="cuda"), torch.randn(k, device="cuda")
+    ups = [thia.thia_linear_i8_load(w1, b1), thia.thia_linear_i8_load(w2, b2)]
+    return ups, [thia.thia_quantize_rows(w) + (b,) for w, b in ((w1, b1), (w2, b2))], 0.5 + torch.rand(k, device="cuda")
+
+
+@pytest.mark.parametrize("rows,k,n", [(1, 256, 1024), (37, 200, 777), (600, 512, 1024), (4096, 256, 512)])
+def test_block(rows, k, n):
+    """Norm, product, codes again and product back onto the sum, as a program chains them; every step against its definition."""
+    (up, down), ((q1, s1, b1), (q2, s2, b2)), gain = block_parts(rows, k, n)
+    x, r = rows_of(3, rows, k, BF), rows_of(4, rows, k, BF)
+    codes, scales, total, u, c2, sc2, out = block(x, r, gain, up, down)
+    h = (x.float() + r.float()).double()
+    check_codes(codes, scales, h * gain.double() / torch.sqrt((h * h).mean(1, keepdim=True) + 1e-6), k, 64)
+    check_product(u, codes, scales, q1[:, :k], s1, b1, k, True)
+    check_codes(c2, sc2, u.double(), n, 2)
+    check_product(out, c2, sc2, q2[:, :n], s2, b2, n, False, total)
+
+
+def test_block_captured_and_on_other_streams():
+    """A captured chain gives the eager results at every replay, on changing inputs and with eager work in between; chains of the
+    same layers on two streams at once do too."""
+    (up, down), _, gain = block_parts(300, 512, 1024)
+    x, r = rows_of(3, 300, 512, BF), rows_of(4, 300, 512, BF)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        block(x, r, gain, up, down)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = block(x, r, gain, up, down)
+    for seed in range(4):
+        x.copy_(rows_of(10 + seed, 300, 512, BF))
+        graph.replay()
+        want = block(x, r, gain, up, down)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want))
+    ys, others = [rows_of(20 + i, 300, 512, BF) for i in range(6)], [torch.cuda.Stream() for _ in range(2)]
+    want = [block(y, r, gain, up, down)[-1] for y in ys]
+    torch.cuda.synchronize()
+    got = []
+    for i, y in enumerate(ys):
+        with torch.cuda.stream(others[i % 2]):
+            got.append(block(y, r, gain, up, down)[-1])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
