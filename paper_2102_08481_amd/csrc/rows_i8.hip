@@ -4,7 +4,7 @@
 //   norm:      h = x (+ r), y = h g / sqrt(mean(h^2) + eps), then the same.  q depends on y's direction alone, so it is h g 127 / max|h g|
 //              whatever the norm is, and one reduction of a row (sum h^2 and max|h g|) gives both the codes and the scale
 //              max|h g| / (127 sqrt(mean + eps)).
-#include "thia_internal.h"
+#include "conv_common.h"
 
 namespace thia {
 
@@ -16,74 +16,187 @@ int i8_fail(int code, const char* why) {
 
 namespace {
 
-__device__ inline float row_load(const float* p) { return *p; }
-__device__ inline float row_load(const bf16_t* p) { return bf16_to_f32(*p); }
-__device__ inline void row_store(float* p, float v) { *p = v; }
-__device__ inline void row_store(bf16_t* p, float v) { *p = (bf16_t)pack_bf16x2(v, 0.f); }
-
-// A row's values from 2^-30 of the largest float down to 2^-100 go the plain way; the others are brought there by a power of two.
-constexpr float kLeast = 7.8886091e-31f, kMost = 3.0e29f;
-
-__device__ inline float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
-
-template <typename Op>
-__device__ inline float block_reduce(float v, Op op, float* red) {
-    for (int o = 32; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = red[0];
-    for (int w = 1; w < (int)blockDim.x / 64; ++w) v = op(v, red[w]);
-    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(v)::"memory");   // red is written again behind the next barrier
-    return v;
+// Eight values side by side; rows need only their element's alignment, which 16-byte accesses of global memory take.
+typedef u32x4_t __attribute__((aligned(2))) u32x4_at2;
+typedef f32x4_t __attribute__((aligned(4))) f32x4_at4;
+__device__ inline void row_load8(const bf16_t* p, float v[8]) { unpack8(Vec8<bf16_t>{*reinterpret_cast<const u32x4_at2*>(p)}, v); }
+__device__ inline void row_load8(const float* p, float v[8]) {
+    unpack8(Vec8<float>{*reinterpret_cast<const f32x4_at4*>(p), *reinterpret_cast<const f32x4_at4*>(p + 4)}, v);
+}
+__device__ inline void row_store8(bf16_t* p, const float v[8]) {
+    const u32x4_t o = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    *reinterpret_cast<u32x4_at2*>(p) = o;
+}
+__device__ inline void row_store8(float* p, const float v[8]) {
+    *reinterpret_cast<f32x4_at4*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f32x4_at4*>(p + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
+}
+// the first n (0..8) of eight values, zeros behind them
+template <typename T>
+__device__ inline void row_load(const T* p, int n, float v[8]) {
+    if (n >= 8) return row_load8(p, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? load_elem(p + j) : 0.f;
+}
+template <typename T>
+__device__ inline void row_store(T* p, int n, const float v[8]) {
+    if (n >= 8) return row_store8(p, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < n) store_elem(p + j, v[j]);
 }
 
-// One row per block.  The maximum of a row with a NaN is made NaN by adding 0 * v, which is 0 for finite v only.
-template <typename T, bool NORM>
-__global__ __launch_bounds__(256) void rows_i8_kernel(const T* x, long long ldx, const T* r, long long ldr, const float* __restrict__ g, float eps,
-                                                      int k, T* sum, long long ldsum, int8_t* __restrict__ codes, int pitch, float* __restrict__ scales) {
-    __shared__ float red[4];
-    const size_t row = blockIdx.x;
-    x += row * ldx;
-    if (NORM && r) r += row * ldr;
-    if (NORM && sum) sum += row * ldsum;
-    codes += row * pitch;
-    auto add = [](float a, float b) { return a + b; };
-    auto most = [](float a, float b) { return fmaxf(a, b); };
-    auto value = [&](int j) { return row_load(x + j) + (NORM && r ? row_load(r + j) : 0.f); };
-    float m = 0.f, bad = 0.f;
-    for (int j = threadIdx.x; j < k; j += 256) {
-        const float h = value(j);
-        m = fmaxf(m, fabsf(h));
-        bad += 0.f * h;
+__device__ inline float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+__device__ inline uint32_t size_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }   // orders |v|, infinity and NaN last
+
+struct RowStat { float ss; uint32_t most; };   // sum of squares, bits of the largest size
+
+struct RowArgs {
+    const void *x, *r;
+    const float* g;
+    void* sum;
+    int8_t* codes;
+    float* scales;
+    long long ldx, ldr, ldsum;
+    float eps;
+    int rows, k, pitch;
+};
+
+// Up to so many pieces of eight per lane the gain stays in registers from row to row; beyond, its registers cost more than its
+// reads from the caches (us, held / read: 9 600 x 1 024 12.8 / 13.9, 16 384 x 4 096 (two pieces) 99 / 119, 4 096 x 16 384 (four) 138 / 109).
+constexpr int kHold = 2;
+// A row per WPR wavefronts, 8 C values of it per lane, in registers from the one load to the codes' store; with WPR 1 four rows
+// per block.  Blocks walk over the rows, so that the gain stays in registers.
+template <typename T, bool NORM, int WPR, int C>
+__global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void rows_i8_kernel(const RowArgs a) {
+    constexpr int RPB = WPR == 1 ? 4 : 1;
+    __shared__ RowStat red[2][WPR];
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int k = a.k;
+    int turn = 0;
+    auto reduce = [&](RowStat s) {
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            s.ss += __shfl_xor(s.ss, o);
+            const uint32_t other = __shfl_xor(s.most, o);
+            s.most = other > s.most ? other : s.most;
+        }
+        if constexpr (WPR > 1) {
+            // two slots in turn: a wavefront that writes one has passed the barrier behind which all have read it
+            if (lane == 0) red[turn][wv] = s;
+            __syncthreads();
+            s = red[turn][0];
+#pragma unroll
+            for (int w = 1; w < WPR; ++w) {
+                const RowStat o = red[turn][w];
+                s.ss += o.ss;
+                s.most = o.most > s.most ? o.most : s.most;
+            }
+            turn ^= 1;
+        }
+        return s;
+    };
+    int at[C], left[C];
+    constexpr bool HOLD = NORM && C <= kHold;
+    float g[HOLD ? C : 1][8];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        at[c] = ((c * WPR + (WPR == 1 ? 0 : wv)) * 64 + lane) * 8;
+        left[c] = k - at[c];
+        if constexpr (HOLD) row_load(a.g + at[c], left[c], g[c]);
     }
-    m = block_reduce(m, most, red);
-    bad = block_reduce(bad, add, red);
-    const bool ok = bad == 0.f && m <= 3.4028235e38f;
-    // exponent that brings the row's largest value to 1..2
-    int e = ok && m > 0.f ? -ilogbf(m) : 0;
-    const float p0 = pow2(e / 2), p1 = pow2(e - e / 2);
-    float ss = 0.f, mg = 0.f;
-    for (int j = threadIdx.x; j < k; j += 256) {
-        const float h = value(j) * p0 * p1;
-        ss += h * h;
-        mg = fmaxf(mg, fabsf(NORM ? h * g[j] : h));
-    }
-    ss = block_reduce(ss, add, red);
-    mg = block_reduce(mg, most, red);
-    const float inv = mg > 0.f ? 127.f / mg : 0.f;
-    for (int j = threadIdx.x; j < pitch; j += 256) {
-        if (j >= k) { codes[j] = 0; continue; }
-        const float h = value(j);
-        if (NORM && sum) row_store(sum + j, h);
-        const float t = NORM ? h * p0 * p1 * g[j] : h * p0 * p1;
-        codes[j] = ok ? (int8_t)rintf(t * inv) : (int8_t)0;
-    }
-    if (threadIdx.x == 0) {
-        double s = (double)mg / 127.0;
-        if (NORM) s /= sqrt((double)ss / k + (double)eps * pow2(e / 2) * pow2(e / 2) * pow2(e - e / 2) * pow2(e - e / 2));
-        else s = s / pow2(e / 2) / pow2(e - e / 2);
-        scales[row] = ok ? (float)s : __uint_as_float(0x7fc00000u);
+    // f(c, gain of the lane's eight values c): held in registers or read again
+    auto gain = [&](auto f) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if constexpr (NORM && !HOLD) {
+                float gc[8];
+                row_load(a.g + at[c], left[c], gc);
+                f(c, gc);
+            } else {
+                f(c, g[HOLD ? c : 0]);
+            }
+        }
+    };
+    for (long long row = (long long)blockIdx.x * RPB + (WPR == 1 ? wv : 0); row < a.rows; row += (long long)gridDim.x * RPB) {
+        const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+        float h[C][8];
+#pragma unroll
+        for (int c = 0; c < C; ++c) row_load(x + at[c], left[c], h[c]);
+        if constexpr (NORM) {
+            if (a.r) {
+                const T* r = static_cast<const T*>(a.r) + row * a.ldr;
+                float v[C][8];
+#pragma unroll
+                for (int c = 0; c < C; ++c) row_load(r + at[c], left[c], v[c]);
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) h[c][j] += v[c][j];
+                if (a.sum) {
+                    T* sum = static_cast<T*>(a.sum) + row * a.ldsum;
+#pragma unroll
+                    for (int c = 0; c < C; ++c) row_store(sum + at[c], left[c], h[c]);
+                }
+            }
+        }
+        auto stat = [&]() {
+            RowStat s = {0.f, 0u};
+            gain([&](int c, const float* gc) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if constexpr (NORM) s.ss += h[c][j] * h[c][j];
+                    const uint32_t b = size_bits(NORM ? h[c][j] * gc[j] : h[c][j]);
+                    s.most = b > s.most ? b : s.most;
+                }
+            });
+            return reduce(s);
+        };
+        RowStat s = stat();
+        float scale;
+        bool ok = true;
+        const float most = __uint_as_float(s.most);
+        if (most >= 1e-30f && most <= 1e30f && (!NORM || (s.ss >= 1e-20f && s.ss <= 1e30f))) {
+            scale = most / 127.f;
+            if constexpr (NORM) scale /= sqrtf(s.ss / (float)k + a.eps);
+        } else {
+            // rows of zeros, of values whose squares or quotients leave fp32, or with a NaN: the row's largest value is brought to 1..2
+            RowStat m = {0.f, 0u};
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t b = size_bits(h[c][j]);
+                    m.most = b > m.most ? b : m.most;
+                }
+            m = reduce(m);
+            ok = m.most < 0x7f800000u;
+            const int e = ok && m.most ? -ilogbf(__uint_as_float(m.most)) : 0;
+            const float p0 = pow2(e / 2), p1 = pow2(e - e / 2);
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[c][j] = h[c][j] * p0 * p1;
+            s = stat();
+            ok = ok && s.most < 0x7f800000u;
+            const double q0 = p0, q1 = p1;
+            double d = (double)__uint_as_float(s.most) / 127.0;
+            if constexpr (NORM) d /= sqrt((double)s.ss / k + (double)a.eps * q0 * q0 * q1 * q1);
+            else d = d / q0 / q1;
+            scale = ok ? (float)d : __uint_as_float(0x7fc00000u);
+        }
+        const float top = __uint_as_float(s.most), inv = ok && top > 0.f ? 127.f / top : 0.f;
+        int8_t* codes = a.codes + (size_t)row * a.pitch;
+        gain([&](int c, const float* gc) {
+            if (at[c] >= a.pitch) return;
+            uint32_t q[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)   // (a product with NaN or infinity is not converted)
+                q[j] = ok ? (uint32_t)(int)rintf((NORM ? h[c][j] * gc[j] : h[c][j]) * inv) & 255u : 0u;
+            const u32x2_t o = {q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24, q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24};
+            *reinterpret_cast<u32x2_t*>(codes + at[c]) = o;
+        });
+        if (lane == 0 && (WPR == 1 || wv == 0)) a.scales[row] = scale;
     }
 }
 
@@ -97,17 +210,31 @@ const char* rows_error(const void* x, long long ldx, int precision, int rows, in
     return nullptr;
 }
 
+template <typename T, bool NORM, int WPR, int C>
+hipError_t launch_cfg(const RowArgs& a, hipStream_t s) {
+    constexpr int RPB = WPR == 1 ? 4 : 1, THREADS = WPR == 1 ? 256 : WPR * 64;
+    const long long groups = ((long long)a.rows + RPB - 1) / RPB, most = 256ll * 2048 / THREADS;   // what the chip holds at once
+    hipLaunchKernelGGL((rows_i8_kernel<T, NORM, WPR, C>), dim3((unsigned)(groups < most ? groups : most)), dim3(THREADS), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T, bool NORM>
+hipError_t launch_rows(const RowArgs& a, hipStream_t s) {
+    const int k = a.k;
+    if (k <= 512) return launch_cfg<T, NORM, 1, 1>(a, s);
+    if (k <= 1024) return launch_cfg<T, NORM, 1, 2>(a, s);
+    if (k <= 2048) return launch_cfg<T, NORM, 4, 1>(a, s);
+    if (k <= 4096) return launch_cfg<T, NORM, 4, 2>(a, s);
+    if (k <= 8192) return launch_cfg<T, NORM, 4, 4>(a, s);
+    if (k <= 16384) return launch_cfg<T, NORM, 8, 4>(a, s);
+    if (k <= 32768) return launch_cfg<T, NORM, 16, 4>(a, s);
+    return launch_cfg<T, NORM, 16, 8>(a, s);
+}
+
 template <bool NORM>
-int launch_rows(const void* x, long long ldx, const void* r, long long ldr, const float* g, float eps, int precision, int rows, int k, void* sum,
-                long long ldsum, int8_t* codes, float* scales, void* stream) {
-    if (rows == 0) return THIA_OK;
-    const hipStream_t s = (hipStream_t)stream;
-    const int pitch = thia_i8_pitch(k);
-    if (precision)
-        hipLaunchKernelGGL((rows_i8_kernel<bf16_t, NORM>), dim3(rows), dim3(256), 0, s, (const bf16_t*)x, ldx, (const bf16_t*)r, ldr, g, eps, k, (bf16_t*)sum, ldsum, codes, pitch, scales);
-    else
-        hipLaunchKernelGGL((rows_i8_kernel<float, NORM>), dim3(rows), dim3(256), 0, s, (const float*)x, ldx, (const float*)r, ldr, g, eps, k, (float*)sum, ldsum, codes, pitch, scales);
-    const hipError_t e = hipGetLastError();
+int launch(const RowArgs& a, int precision, void* stream) {
+    if (a.rows == 0) return THIA_OK;
+    const hipError_t e = precision ? launch_rows<bf16_t, NORM>(a, (hipStream_t)stream) : launch_rows<float, NORM>(a, (hipStream_t)stream);
     return e == hipSuccess ? THIA_OK : i8_fail(THIA_E_HIP, hipGetErrorString(e));
 }
 
@@ -125,7 +252,7 @@ int thia_i8_pitch(int k) { return k < 1 || k > kMaxI8Cols ? 0 : (k + 127) / 128 
 int thia_quantize_rows(const void* x, long long ldx, int precision, int rows, int k, int8_t* codes, float* scales, void* hip_stream) {
     if (const char* why = rows_error(x, ldx, precision, rows, k, codes, scales)) return i8_fail(THIA_E_BADARG, why);
     if (k > kMaxI8Cols) return i8_fail(THIA_E_SHAPE, "more than 65536 columns");
-    return launch_rows<false>(x, ldx, nullptr, 0, nullptr, 0.f, precision, rows, k, nullptr, 0, codes, scales, hip_stream);
+    return launch<false>({x, nullptr, nullptr, nullptr, codes, scales, ldx, 0, 0, 0.f, rows, k, thia_i8_pitch(k)}, precision, hip_stream);
 }
 
 int thia_rms_norm_i8(const void* x, long long ldx, const void* residual, long long ldr, const float* gain, float eps, int precision, int rows, int k,
@@ -138,7 +265,7 @@ int thia_rms_norm_i8(const void* x, long long ldx, const void* residual, long lo
     const uintptr_t elem = precision ? 2 : 4;
     if ((uintptr_t)residual % elem || (uintptr_t)sum % elem || (uintptr_t)gain % 4) return i8_fail(THIA_E_BADARG, "misaligned pointer");
     if (k > kMaxI8Cols) return i8_fail(THIA_E_SHAPE, "more than 65536 columns");
-    return launch_rows<true>(x, ldx, residual, ldr, gain, eps, precision, rows, k, sum, ldsum, codes, scales, hip_stream);
+    return launch<true>({x, residual, gain, sum, codes, scales, ldx, ldr, ldsum, eps, rows, k, thia_i8_pitch(k)}, precision, hip_stream);
 }
 
 }  // extern "C"
