@@ -5,6 +5,8 @@
 // Weights lie in matrix-instruction fragments: for every 32 channels and 32 k one contiguous 1 KiB in which lane l's 16 bytes are
 // v[32 ct + l % 32][32 ks + 16 (l / 32) .. + 15]; rows and k behind the last are zeros, so what an activation row holds behind
 // column k does not matter.
+#include <math.h>
+
 #include <new>
 
 #include "conv_common.h"
@@ -32,6 +34,7 @@ struct LinearArgs {
     void* out;
     long long ldr, ldo;
     int rows, n, pitch, relu;
+    int vec;   // rows of out and res take accesses of 16 bytes: n a multiple of 8, addresses and pitches of 16 bytes
 };
 
 // int8 rows [n][ld] -> fragments; one thread per 16 bytes
@@ -48,39 +51,143 @@ __global__ void pack_i8_kernel(const int8_t* __restrict__ src, long long ld, int
     *reinterpret_cast<i32x4_t*>(dst + p * 16) = o.v;
 }
 
-// What a lane does with one sum: channel ch of row m.  ReLU keeps a NaN.
+__device__ inline __amdgpu_buffer_rsrc_t buffer(const void* p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
+}
+__device__ inline i32x16_t mma_i8(const u32x4_t& w, const u32x4_t& x, const i32x16_t& acc) {
+    return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4_t, w), __builtin_bit_cast(i32x4_t, x), acc, 0, 0, 0);
+}
+// ReLU that keeps a NaN.
+__device__ inline float relu_if(bool relu, float v) { return relu && v < 0.f ? 0.f : v; }
+
+// ---- epilogue of the smaller tiles: four channels from ch (a multiple of 4) on of row m, if it exists.
 template <typename T>
-__device__ inline float finish(const LinearArgs& a, int acc, float xs, size_t m, int ch) {
-    float v = ((float)acc * xs) * a.wscale[ch] + a.bias[ch];
-    if (a.res) v += load_elem(static_cast<const T*>(a.res) + m * a.ldr + ch);
-    return a.relu && v < 0.f ? 0.f : v;
+__device__ inline void finish_four(const LinearArgs& a, const i32x4_t& s, size_t m, bool exists, int ch) {
+    if (!exists || ch >= a.n) return;
+    const float xs = a.xscale[m];
+    const f32x4_t ws = *reinterpret_cast<const f32x4_t*>(a.wscale + ch), b = *reinterpret_cast<const f32x4_t*>(a.bias + ch);
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = ((float)s[e] * xs) * ws[e] + b[e];
+    T* out = static_cast<T*>(a.out) + m * a.ldo + ch;
+    const T* res = a.res ? static_cast<const T*>(a.res) + m * a.ldr + ch : nullptr;
+    if (a.vec) {
+        if (res) {
+            float r[4];
+            load4(res, r);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += r[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = relu_if(a.relu, v[e]);
+        store4(out, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (ch + e < a.n) store_elem(out + e, relu_if(a.relu, v[e] + (res ? load_elem(res + e) : 0.f)));
+    }
 }
 
-// One wavefront per 32 rows x 32 channels, fragments straight from memory.
-template <typename T>
-__global__ __launch_bounds__(64) void linear_i8_kernel(const LinearArgs a) {
-    const int lane = threadIdx.x;
-    const size_t m = (size_t)blockIdx.x * 32 + (lane & 31);
-    const int ct = blockIdx.y;
-    const bool ok = m < (size_t)a.rows;
-    const i32x4_t* w = reinterpret_cast<const i32x4_t*>(a.w + (size_t)ct * 32 * a.pitch) + lane;
-    const int8_t* x = a.x + (ok ? m : 0) * a.pitch + (lane >> 5) * 16;
-    i32x16_t acc = {};
-    for (int ks = 0; ks < a.pitch / 32; ++ks)
-        acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[(size_t)ks * 64], *reinterpret_cast<const i32x4_t*>(x + ks * 32), acc, 0, 0, 0);
-    if (!ok) return;
-    const float xs = a.xscale[m];
+// ---- epilogue of the larger tiles: a wavefront's 32 TM rows x 64 channels.  Sum e of lane l: channel 8 (e / 4) + 4 (l / 32) + e % 4, row
+// l % 32.  32 rows at a time are parked in the wavefront's own FINISH_LDS bytes of LDS and read back by rows, so that accesses
+// of memory cover whole lines.  m0 + r0: the wavefront's first row; `rows` of the block's rows exist; nw: the first channel.
+constexpr int FINISH_PITCH = 64 * 4 + 16, FINISH_LDS = 32 * FINISH_PITCH;
+template <typename T, int TM>
+__device__ inline void finish_rows(const LinearArgs& a, const i32x16_t (&acc)[2][TM], unsigned char* ep, int lane, size_t m0, int r0, int rows, int nw) {
+    const int frag_row = lane & 31;
+    f32x4_t ws[2][4], bs[2][4];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        const int ch = ct * 32 + 8 * (e / 4) + 4 * (lane >> 5) + e % 4;
-        if (ch < a.n) store_elem(static_cast<T*>(a.out) + m * a.ldo + ch, finish<T>(a, acc[e], xs, m, ch));
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {   // (scales and biases have room for whole blocks)
+            ws[i][v] = *reinterpret_cast<const f32x4_t*>(a.wscale + nw + i * 32 + 8 * v + 4 * (lane >> 5));
+            bs[i][v] = *reinterpret_cast<const f32x4_t*>(a.bias + nw + i * 32 + 8 * v + 4 * (lane >> 5));
+        }
+    static_for<0, TM>([&](auto jc) {
+        constexpr int j = decltype(jc)::value;
+        const int rj = r0 + j * 32;
+        const float xs = rj + frag_row < rows ? a.xscale[m0 + rj + frag_row] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                f32x4_t r;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) r[e] = ((float)acc[i][j][4 * v + e] * xs) * ws[i][v][e] + bs[i][v][e];
+                *reinterpret_cast<f32x4_t*>(ep + (size_t)frag_row * FINISH_PITCH + (i * 32 + 8 * v + 4 * (lane >> 5)) * 4) = r;
+            }
+        __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the region is private to this wavefront
+        __builtin_amdgcn_wave_barrier();
+        if (a.vec) {
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {   // eight lanes per row
+                const int r = it * 8 + (lane >> 3), c = (lane & 7) * 8;
+                if (rj + r >= rows || nw + c >= a.n) continue;
+                float o[8], y[8];
+                unpack8(*reinterpret_cast<const Vec8<float>*>(ep + (size_t)r * FINISH_PITCH + c * 4), o);
+                if (a.res) {
+                    unpack8(*reinterpret_cast<const Vec8<T>*>(static_cast<const T*>(a.res) + (m0 + rj + r) * a.ldr + nw + c), y);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] += y[e];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = relu_if(a.relu, o[e]);
+                store8(static_cast<T*>(a.out) + (m0 + rj + r) * a.ldo + nw + c, o);
+            }
+        } else if (nw + lane < a.n) {
+            for (int r = 0; r < 32 && rj + r < rows; ++r) {
+                const size_t m = m0 + rj + r;
+                float o = *reinterpret_cast<const float*>(ep + (size_t)r * FINISH_PITCH + lane * 4);
+                if (a.res) o += load_elem(static_cast<const T*>(a.res) + m * a.ldr + nw + lane);
+                store_elem(static_cast<T*>(a.out) + m * a.ldo + nw + lane, relu_if(a.relu, o));
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+        __builtin_amdgcn_wave_barrier();
+    });
+}
+
+#include "linear_i8_large.h"
+#include "linear_i8_mid.h"
+#include "linear_i8_small.h"
+#include "linear_i8_tiny.h"
+
+// Which tile: the one with the least base + rounds * K tiles * per_k + max(1, tiles / 256) * per_tile, in us, `rounds` the tiles that one
+// of the 256 CUs gets (ceil).  The constants are a least-squares fit (relative errors) to 120 shapes of 1 to 16 384 rows, 128 to 12 544
+// columns and 64 to 8 192 channels; over these the rule is 0.7 % from the best of the seven in the geometric mean, 22 % at worst (a call of 3 us).
+// us, 16 x 16 / 32 x 32 / 32 x 64 / 64 x 64 / 128 x 128 / 192 x 256 / 256 x 256 (rows x columns x channels): 1 x 4096 x 4096 3.9 / 4.7 / 5.5 / 7.0 / - / - / -;
+// 130 x 4096 x 512 7.5 / 4.8 / 5.9 / 7.9 / 19 / 31 / 38; 700 x 256 x 2048 9.0 / 6.3 / 4.9 / 5.6 / 7.9 / 10.1 / 12.1; 1000 x 12544 x 1024 - / 57 / - / 24 / 46 / 78 / 94;
+// 4000 x 1024 x 1024 - / 21 / 15.6 / 15.1 / 11.7 / 15.5 / 18.2; 9600 x 12544 x 1024 128 x 128 165, 107 / 117; 8192 x 8192 x 8192 707, 502 / 445.
+struct Tile { int rows, chans; double base, per_k, per_tile; };
+constexpr Tile kTiles[] = {{16, 16, 2.66, 0.070, 0.186}, {32, 32, 2.54, 0.063, 0.566}, {32, 64, 2.60, 0.088, 0.784}, {64, 64, 2.39, 0.118, 1.806},
+                           {128, 128, 0.0, 0.452, 6.995}, {192, 256, 0.0, 0.743, 9.045}, {256, 256, 0.0, 0.947, 10.537}};
+
+int choose_tile(int rows, int n, int pitch) {
+    int best = 0;
+    double least = 0.0;
+    for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
+        const Tile& t = kTiles[i];
+        if (t.chans == 256 && pitch < 256) continue;   // two K tiles are under way there
+        const double tiles = (double)((rows + (long long)t.rows - 1) / t.rows) * ((n + t.chans - 1) / t.chans);
+        double per_k = t.per_k;
+        if (i == 0) per_k *= 0.5 + 0.03125 * (rows < 16 ? rows : 16);   // rows that do not exist are not fetched
+        const double us = t.base + ceil(tiles / 256) * (pitch / 128) * per_k + (tiles > 256 ? tiles / 256 : 1.0) * t.per_tile;
+        if (i == 0 || us < least) { best = i; least = us; }
     }
+    return best;
 }
 
 template <typename T>
 hipError_t launch_linear(const LinearArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL(linear_i8_kernel<T>, dim3((a.rows + 31) / 32, up(a.n, 32) / 32), dim3(64), 0, s, a);
-    return hipGetLastError();
+    switch (choose_tile(a.rows, a.n, a.pitch)) {
+        case 0: return launch_tiny<T, 4>(a, s);
+        case 1: return launch_small<T, 1, 1, 4, 2>(a, s);
+        case 2: return launch_small<T, 1, 2, 4, 1>(a, s);
+        case 3: return launch_small<T, 2, 2, 4, 1>(a, s);
+        case 4: return launch_mid<T, 128, 128, 4>(a, s);
+        case 5: return launch_large<T, 192>(a, s);
+        default: return launch_large<T, 256>(a, s);
+    }
 }
 
 // Weights as rows of codes on the device -> the layer's fragments, scales and biases; waits for the device's work.
@@ -188,8 +295,19 @@ int thia_linear_i8_run(const thia_linear_i8* l, const int8_t* codes, const float
     if (e != hipSuccess) return i8_fail(THIA_E_HIP, hipGetErrorString(e));
     if (dev != l->device) return i8_fail(THIA_E_BADARG, "the layer lies on another device than the current one");
     if (rows == 0) return THIA_OK;
-    LinearArgs a = {l->w, l->scale_bias, l->scale_bias + up(l->n, 256), codes, scales, residual, out, ldr, ldo, rows, l->n, l->pitch, relu != 0};
-    e = precision ? launch_linear<bf16_t>(a, (hipStream_t)hip_stream) : launch_linear<float>(a, (hipStream_t)hip_stream);
+    LinearArgs a = {l->w, l->scale_bias, l->scale_bias + up(l->n, 256), codes, scales, residual, out, ldr, ldo, rows, l->n, l->pitch, relu != 0, 0};
+    const auto wide = [&](const void* p, long long ld) { return (uintptr_t)p % 16 == 0 && ld * (long long)elem % 16 == 0; };
+    a.vec = l->n % 8 == 0 && wide(out, ldo) && (!residual || wide(residual, ldr));
+    // rows in as many launches as keep the number of threads of each below 2^32 (a multiple of every tile's rows)
+    const int most = (int)((1ll << 33) / l->n / 768 < 2048 ? (1ll << 33) / l->n / 768 : 2048) * 768;
+    for (long long m = 0; m < rows && e == hipSuccess; m += most) {
+        a.rows = rows - m < most ? (int)(rows - m) : most;
+        a.x = codes + m * l->pitch;
+        a.xscale = scales + m;
+        a.res = residual ? static_cast<const char*>(residual) + m * ldr * (long long)elem : nullptr;
+        a.out = static_cast<char*>(out) + m * ldo * (long long)elem;
+        e = precision ? launch_linear<bf16_t>(a, (hipStream_t)hip_stream) : launch_linear<float>(a, (hipStream_t)hip_stream);
+    }
     return e == hipSuccess ? THIA_OK : i8_fail(THIA_E_HIP, hipGetErrorString(e));
 }
 
