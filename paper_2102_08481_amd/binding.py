@@ -556,84 +556,84 @@ class Classifier:
 _I8_TYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
-def _i8_check(rc):
+def _i8_call(device, call, *args):
+    """One call on torch's current stream of `device`.  (A call is a few us on the device: the device is switched, and the stream
+    asked for, in the cheapest way there is.)"""
+    index = device.index
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    if index == torch.cuda.current_device():
+        rc = call(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            rc = call(*args, stream)
     if rc:
         raise ThiaError(rc, lib().thia_i8_last_error().decode())
 
 
 def _i8_rows(name, t, dtype, device, shape):
-    """Tensor argument as (pointer, row pitch): [rows, k] with dense rows, any pitch; None passes."""
-    if t is None:
-        return None, 0
-    if t.device != device or t.dtype != dtype or tuple(t.shape) != shape:
+    """Row pitch of a tensor argument: [rows, k] with dense rows, any pitch."""
+    if t.dtype is not dtype or t.shape != shape or t.device != device:
         raise ValueError(f"{name} must be {dtype} {list(shape)} on {device}, not {t.dtype} {list(t.shape)} on {t.device}")
+    ld, step = t.stride()
     rows, k = shape
-    if (k > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < k):
+    if (step != 1 and k > 1) or (ld < k and rows > 1):
         raise ValueError(f"{name}: the values of a row must lie side by side and rows must not overlap")
-    return t.data_ptr(), t.stride(0) if rows > 1 else k
+    return ld if rows > 1 else k
 
 
 def _i8_vector(name, t, n, device):
-    if t.device != device or t.dtype != torch.float32 or tuple(t.shape) != (n,) or not t.is_contiguous():
+    if t.dtype is not torch.float32 or t.shape != (n,) or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a dense float32 [{n}] on {device}")
-    return t.data_ptr()
 
 
-def _i8_input(x):
-    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == 2 and x.dtype in _I8_TYPES):
-        raise ValueError("rows must be a two-dimensional float32 or bfloat16 tensor on the GPU")
-    return x.shape[0], x.shape[1], x.device
-
-
-def _i8_codes(rows, k, device, out):
-    """Codes and scales to write, new or given, as (codes, scales)."""
-    pitch = lib().thia_i8_pitch(k)
-    if not pitch:
-        raise ThiaError(-3, "rows of codes hold 1 to 65536 values")
-    if out is None:
-        return torch.empty((rows, pitch), dtype=torch.int8, device=device), torch.empty(rows, dtype=torch.float32, device=device)
-    codes, scales = out
-    _i8_given(codes, scales, rows, pitch, device)
-    return codes, scales
-
-
-def _i8_given(codes, scales, rows, pitch, device):
-    if codes.device != device or codes.dtype != torch.int8 or tuple(codes.shape) != (rows, pitch) or not codes.is_contiguous():
+def _i8_codes(codes, scales, rows, pitch, device):
+    if codes.dtype is not torch.int8 or codes.shape != (rows, pitch) or codes.device != device or not codes.is_contiguous():
         raise ValueError(f"codes must be dense int8 [{rows}, {pitch}] on {device}")
     _i8_vector("scales", scales, rows, device)
 
 
-def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
+def _i8_start(x, out):
+    """What rows x become: (precision, row pitch, rows, k, device, codes, scales), the last two new or given."""
+    precision = _I8_TYPES.get(x.dtype) if isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == 2 else None
+    if precision is None:
+        raise ValueError("rows must be a two-dimensional float32 or bfloat16 tensor on the GPU")
+    device, (rows, k) = x.device, x.shape
+    ldx = _i8_rows("x", x, x.dtype, device, x.shape)
+    if not 1 <= k <= 65536:
+        raise ThiaError(-3, "rows of codes hold 1 to 65536 values")
+    pitch = -(-k // 128) * 128
+    if out is None:
+        return precision, ldx, rows, k, device, torch.empty((rows, pitch), dtype=torch.int8, device=device), torch.empty(rows, dtype=torch.float32, device=device)
+    _i8_codes(*out, rows, pitch, device)
+    return (precision, ldx, rows, k, device, *out)
 
 
 def quantize_rows(x, out=None):
     """x: float32 / bfloat16 cuda [rows, k] (dense rows, any pitch) -> (codes int8 [rows, pitch], scales float32 [rows]), on torch's
     current stream; out: such a pair to write into."""
-    rows, k, device = _i8_input(x)
-    xp, ldx = _i8_rows("x", x, x.dtype, device, (rows, k))
-    codes, scales = _i8_codes(rows, k, device, out)
-    with torch.cuda.device(device):
-        _i8_check(lib().thia_quantize_rows(xp, ldx, _I8_TYPES[x.dtype], rows, k, codes.data_ptr(), scales.data_ptr(), _stream(device)))
+    precision, ldx, rows, k, device, codes, scales = _i8_start(x, out)
+    _i8_call(device, lib().thia_quantize_rows, x.data_ptr(), ldx, precision, rows, k, codes.data_ptr(), scales.data_ptr())
     return codes, scales
 
 
 def rms_norm_i8(x, gain, eps=1e-6, residual=None, sum_out=None, out=None):
     """Norm of x + residual in 8 bits: (codes, scales, sum), sum = x + residual in x's type (None without a residual).  sum_out: where
     it goes (may be x or residual); out: (codes, scales) to write into."""
-    rows, k, device = _i8_input(x)
-    xp, ldx = _i8_rows("x", x, x.dtype, device, (rows, k))
-    rp, ldr = _i8_rows("residual", residual, x.dtype, device, (rows, k))
-    gp = _i8_vector("gain", gain, k, device)
-    if residual is None and sum_out is not None:
+    precision, ldx, rows, k, device, codes, scales = _i8_start(x, out)
+    _i8_vector("gain", gain, k, device)
+    rp = sp = None
+    ldr = lds = k
+    if residual is not None:
+        ldr, rp = _i8_rows("residual", residual, x.dtype, device, x.shape), residual.data_ptr()
+        if sum_out is None:
+            sum_out = torch.empty((rows, k), dtype=x.dtype, device=device)
+        else:
+            lds = _i8_rows("sum_out", sum_out, x.dtype, device, x.shape)
+        sp = sum_out.data_ptr()
+    elif sum_out is not None:
         raise ValueError("a sum without a residual")
-    if residual is not None and sum_out is None:
-        sum_out = torch.empty((rows, k), dtype=x.dtype, device=device)
-    sp, lds = _i8_rows("sum_out", sum_out, x.dtype, device, (rows, k))
-    codes, scales = _i8_codes(rows, k, device, out)
-    with torch.cuda.device(device):
-        _i8_check(lib().thia_rms_norm_i8(xp, ldx, rp, ldr, gp, eps, _I8_TYPES[x.dtype], rows, k, sp, lds, codes.data_ptr(), scales.data_ptr(),
-                                         _stream(device)))
+    _i8_call(device, lib().thia_rms_norm_i8, x.data_ptr(), ldx, rp, ldr, gain.data_ptr(), eps, precision, rows, k, sp, lds, codes.data_ptr(),
+             scales.data_ptr())
     return codes, scales, sum_out
 
 
@@ -667,7 +667,8 @@ class LinearI8:
                 rc = lib().thia_linear_i8_load(ptr(w), ptr(b), self.n, self.k, C.byref(h))
             else:
                 rc = lib().thia_linear_i8_load_codes(ptr(w), ptr(s), ptr(b), self.n, self.k, C.byref(h))
-        _i8_check(rc)
+        if rc:
+            raise ThiaError(rc, lib().thia_i8_last_error().decode())
         self._h = h
 
     def run(self, codes, scales, relu=False, residual=None, out_f32=False, out=None):
@@ -675,15 +676,17 @@ class LinearI8:
         residual: [rows, n] of that type, added in front of the ReLU; out: where the result goes (may be residual)."""
         if self._h is None:
             raise ThiaError(-1, "the layer has been freed")
-        rows, dtype = scales.shape[0] if scales.dim() == 1 else -1, torch.float32 if out_f32 else torch.bfloat16
-        _i8_given(codes, scales, rows, self.pitch, self.device)
+        device, rows, dtype = self.device, scales.numel(), torch.float32 if out_f32 else torch.bfloat16
+        _i8_codes(codes, scales, rows, self.pitch, device)
+        rp, ldr, ldo = None, self.n, self.n
+        if residual is not None:
+            ldr, rp = _i8_rows("residual", residual, dtype, device, (rows, self.n)), residual.data_ptr()
         if out is None:
-            out = torch.empty((rows, self.n), dtype=dtype, device=self.device)
-        rp, ldr = _i8_rows("residual", residual, dtype, self.device, (rows, self.n))
-        op, ldo = _i8_rows("out", out, dtype, self.device, (rows, self.n))
-        with torch.cuda.device(self.device):
-            _i8_check(lib().thia_linear_i8_run(self._h, codes.data_ptr(), scales.data_ptr(), rows, rp, ldr, int(relu), int(not out_f32), op,
-                                               ldo, _stream(self.device)))
+            out = torch.empty((rows, self.n), dtype=dtype, device=device)
+        else:
+            ldo = _i8_rows("out", out, dtype, device, (rows, self.n))
+        _i8_call(device, lib().thia_linear_i8_run, self._h, codes.data_ptr(), scales.data_ptr(), rows, rp, ldr, 1 if relu else 0, 0 if out_f32 else 1,
+                 out.data_ptr(), ldo)
         return out
 
     def close(self):
