@@ -63,7 +63,7 @@ struct RowArgs {
 };
 
 // Up to so many pieces of eight per lane the gain stays in registers from row to row; beyond, its registers cost more than its
-// reads from the caches (us, held / read: 9 600 x 1 024 12.8 / 13.9, 16 384 x 4 096 (two pieces) 99 / 119, 4 096 x 16 384 (four) 138 / 109).
+// reads from the caches (us, held / read: 9 600 x 1 024 12.8 / 13.9, 16 384 x 4 096 in two pieces 99 / 119, 4 096 x 16 384 in four 138 / 109).
 constexpr int kHold = 2;
 // A row per WPR wavefronts, 8 C values of it per lane, in registers from the one load to the codes' store; with WPR 1 four rows
 // per block.  Blocks walk over the rows, so that the gain stays in registers.
@@ -213,20 +213,26 @@ const char* rows_error(const void* x, long long ldx, int precision, int rows, in
 template <typename T, bool NORM, int WPR, int C>
 hipError_t launch_cfg(const RowArgs& a, hipStream_t s) {
     constexpr int RPB = WPR == 1 ? 4 : 1, THREADS = WPR == 1 ? 256 : WPR * 64;
-    const long long groups = ((long long)a.rows + RPB - 1) / RPB, most = 256ll * 2048 / THREADS;   // what the chip holds at once
+    // Blocks that the chip holds at once walk over the rows; without a gain to keep, a wide row is a block of its own, so that a last
+    // round is not waited for (us, walking / a block per row: norm of 8 192 x 8 192 91 / 105, codes of 9 600 x 12 544 103 / 93).
+    const long long groups = ((long long)a.rows + RPB - 1) / RPB, most = !NORM && WPR > 1 ? 1 << 22 : 256ll * 2048 / THREADS;
     hipLaunchKernelGGL((rows_i8_kernel<T, NORM, WPR, C>), dim3((unsigned)(groups < most ? groups : most)), dim3(THREADS), 0, s, a);
     return hipGetLastError();
 }
 
+// Up to 1024 values a wavefront per row, which needs no barrier (9 600 x 1 024 norm in us: one wavefront 13.1, two 13.5, four
+// 16.3).  Beyond, a row is spread until a lane has eight values of it for the norm, which holds most registers (us, 8 / 16 / 32 values per
+// lane: 16 384 x 4 096 91 / 98 / 126, 8 192 x 8 192 91 / 96 / 111), and sixteen or 32 without it (8 192 x 8 192 38 / 35 / 35, 16 384 x 4 096 36 / 32 /
+// 34); with few rows the wider spread is the quicker too (one row of 8 192: norm 4.4 / 4.4 / 6.1, codes 3.4 / 3.4 / 3.9).
 template <typename T, bool NORM>
 hipError_t launch_rows(const RowArgs& a, hipStream_t s) {
     const int k = a.k;
     if (k <= 512) return launch_cfg<T, NORM, 1, 1>(a, s);
     if (k <= 1024) return launch_cfg<T, NORM, 1, 2>(a, s);
     if (k <= 2048) return launch_cfg<T, NORM, 4, 1>(a, s);
-    if (k <= 4096) return launch_cfg<T, NORM, 4, 2>(a, s);
-    if (k <= 8192) return launch_cfg<T, NORM, 4, 4>(a, s);
-    if (k <= 16384) return launch_cfg<T, NORM, 8, 4>(a, s);
+    if (k <= 4096) return launch_cfg<T, NORM, NORM ? 8 : 4, NORM ? 1 : 2>(a, s);
+    if (k <= 8192) return launch_cfg<T, NORM, NORM ? 16 : 8, NORM ? 1 : 2>(a, s);
+    if (k <= 16384) return launch_cfg<T, NORM, NORM ? 16 : 8, NORM ? 2 : 4>(a, s);
     if (k <= 32768) return launch_cfg<T, NORM, 16, 4>(a, s);
     return launch_cfg<T, NORM, 16, 8>(a, s);
 }
