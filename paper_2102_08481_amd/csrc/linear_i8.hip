@@ -209,23 +209,46 @@ int fill_layer(thia_linear_i8* l, const int8_t* codes, long long ld, const float
     return e == hipSuccess ? THIA_OK : i8_fail(THIA_E_HIP, hipGetErrorString(e));
 }
 
-int new_layer(const void* weights, int n, int k, thia_linear_i8** out, thia_linear_i8** l) {
-    if (out) *out = nullptr;
+int layer_error(const void* weights, int n, int k, thia_linear_i8** out) {
     if (!weights || !out) return i8_fail(THIA_E_BADARG, "null pointer");
     if (n < 1 || k < 1) return i8_fail(THIA_E_BADARG, "a layer has channels and columns");
     if (k > kMaxI8Cols || n > kMaxI8Channels) return i8_fail(THIA_E_SHAPE, "more than 65536 columns or 2^20 channels");
-    *l = new (std::nothrow) thia_linear_i8;
-    if (!*l) return i8_fail(THIA_E_NOMEM, "out of host memory");
-    (*l)->n = n;
-    (*l)->k = k;
-    (*l)->pitch = thia_i8_pitch(k);
-    const hipError_t e = hipGetDevice(&(*l)->device);
-    if (e == hipSuccess) return THIA_OK;
-    delete *l;
-    return i8_fail(THIA_E_HIP, hipGetErrorString(e));
+    return THIA_OK;
+}
+
+// A layer of codes [n][ld] on the device; `out` is set if it succeeds.
+int new_layer(const int8_t* codes, long long ld, const float* scales, const float* bias, int n, int k, thia_linear_i8** out) {
+    thia_linear_i8* l = new (std::nothrow) thia_linear_i8;
+    if (!l) return i8_fail(THIA_E_NOMEM, "out of host memory");
+    l->n = n;
+    l->k = k;
+    l->pitch = thia_i8_pitch(k);
+    const hipError_t e = hipGetDevice(&l->device);
+    const int rc = e == hipSuccess ? fill_layer(l, codes, ld, scales, bias) : i8_fail(THIA_E_HIP, hipGetErrorString(e));
+    if (rc != THIA_OK) thia_linear_i8_free(l);
+    else *out = l;
+    return rc;
 }
 
 }  // namespace
+
+// the channels' codes and scales are those of thia_quantize_rows
+int linear_i8_from_rows(const void* rows, int precision, const float* bias, int n, int k, thia_linear_i8** out) {
+    if (const int rc = layer_error(rows, n, k, out)) return rc;
+    const int pitch = thia_i8_pitch(k);
+    const size_t codes = (size_t)n * pitch;   // (a multiple of 128)
+    void* tmp = nullptr;
+    if (hipMalloc(&tmp, codes + (size_t)n * 4) != hipSuccess) {
+        (void)hipGetLastError();
+        return i8_fail(THIA_E_NOMEM, "weights do not fit the device");
+    }
+    float* scales = reinterpret_cast<float*>(static_cast<char*>(tmp) + codes);
+    int rc = thia_quantize_rows(rows, k, precision, n, k, static_cast<int8_t*>(tmp), scales, nullptr);
+    if (rc == THIA_OK) rc = new_layer(static_cast<int8_t*>(tmp), pitch, scales, bias, n, k, out);
+    (void)hipFree(tmp);
+    return rc;
+}
+
 }  // namespace thia
 
 using namespace thia;
@@ -240,45 +263,31 @@ void thia_linear_i8_free(thia_linear_i8* l) {
 }
 
 int thia_linear_i8_load(const float* weights, const float* bias, int n, int k, thia_linear_i8** out) {
-    thia_linear_i8* l = nullptr;
-    int rc = new_layer(weights, n, k, out, &l);
-    if (rc != THIA_OK) return rc;
-    // the channels' codes and scales are those of thia_quantize_rows
+    if (out) *out = nullptr;
+    if (const int rc = layer_error(weights, n, k, out)) return rc;
     void* tmp = nullptr;
-    const size_t raw = (size_t)n * k * 4, codes = (size_t)n * l->pitch, at_codes = (raw + 255) / 256 * 256, at_scales = at_codes + codes;
-    if (hipMalloc(&tmp, at_scales + (size_t)n * 4) != hipSuccess) {
+    if (hipMalloc(&tmp, (size_t)n * k * 4) != hipSuccess) {
         (void)hipGetLastError();
-        rc = i8_fail(THIA_E_NOMEM, "weights do not fit the device");
-    } else {
-        int8_t* c = static_cast<int8_t*>(tmp) + at_codes;
-        float* s = reinterpret_cast<float*>(static_cast<char*>(tmp) + at_scales);
-        const hipError_t e = hipMemcpy(tmp, weights, raw, hipMemcpyDefault);
-        rc = e == hipSuccess ? thia_quantize_rows(tmp, k, 0, n, k, c, s, nullptr) : i8_fail(THIA_E_HIP, hipGetErrorString(e));
-        if (rc == THIA_OK) rc = fill_layer(l, c, l->pitch, s, bias);
-        (void)hipFree(tmp);
+        return i8_fail(THIA_E_NOMEM, "weights do not fit the device");
     }
-    if (rc != THIA_OK) thia_linear_i8_free(l);
-    else *out = l;
+    const hipError_t e = hipMemcpy(tmp, weights, (size_t)n * k * 4, hipMemcpyDefault);
+    const int rc = e == hipSuccess ? linear_i8_from_rows(tmp, 0, bias, n, k, out) : i8_fail(THIA_E_HIP, hipGetErrorString(e));
+    (void)hipFree(tmp);
     return rc;
 }
 
 int thia_linear_i8_load_codes(const int8_t* codes, const float* scales, const float* bias, int n, int k, thia_linear_i8** out) {
     if (out) *out = nullptr;
     if (!scales) return i8_fail(THIA_E_BADARG, "null pointer");
-    thia_linear_i8* l = nullptr;
-    int rc = new_layer(codes, n, k, out, &l);
-    if (rc != THIA_OK) return rc;
+    if (const int rc = layer_error(codes, n, k, out)) return rc;
     void* tmp = nullptr;
     if (hipMalloc(&tmp, (size_t)n * k) != hipSuccess) {
         (void)hipGetLastError();
-        rc = i8_fail(THIA_E_NOMEM, "weights do not fit the device");
-    } else {
-        const hipError_t e = hipMemcpy(tmp, codes, (size_t)n * k, hipMemcpyDefault);
-        rc = e == hipSuccess ? fill_layer(l, static_cast<int8_t*>(tmp), k, scales, bias) : i8_fail(THIA_E_HIP, hipGetErrorString(e));
-        (void)hipFree(tmp);
+        return i8_fail(THIA_E_NOMEM, "weights do not fit the device");
     }
-    if (rc != THIA_OK) thia_linear_i8_free(l);
-    else *out = l;
+    const hipError_t e = hipMemcpy(tmp, codes, (size_t)n * k, hipMemcpyDefault);
+    const int rc = e == hipSuccess ? new_layer(static_cast<int8_t*>(tmp), k, scales, bias, n, k, out) : i8_fail(THIA_E_HIP, hipGetErrorString(e));
+    (void)hipFree(tmp);
     return rc;
 }
 

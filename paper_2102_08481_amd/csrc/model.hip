@@ -45,6 +45,7 @@ struct ExitUnit {
     bf16_t* head_f = nullptr;
     float* head_fb = nullptr;
     bf16_t* lat_f = nullptr;   // lateral 256 -> 256 in fragment order (tail layer of the 64-wide stage's last block); else null
+    thia_linear_i8 *fc1_i8 = nullptr, *fc2_i8 = nullptr;   // the wide layers in 8 bits (thia_set_head_bits), once asked for
 };
 
 struct Tap {
@@ -66,6 +67,8 @@ struct Workspace {
     void *roi_feat = nullptr, *h1 = nullptr, *h2 = nullptr;
     float *cls = nullptr, *box = nullptr, *cand_scores = nullptr, *cand_boxes = nullptr;
     int key_cap = 0;
+    int8_t* codes = nullptr;        // 8-bit rows of the box head and their scales; null unless asked for
+    float* code_scales = nullptr;
 };
 
 }  // namespace
@@ -88,6 +91,7 @@ struct thia_model {
     int user_mb = 0;
     bool fuse_blocks = true;  // identity bottlenecks as one kernel where a variant exists
     bool fuse_always = false; // take fused variants also below the sizes where they pay (tests)
+    int head_bits = 0;        // 8: the box head's wide layers multiply in 8 bits
     // exit estimator (two layers on the pooled last-stage features); est_hidden == 0: none set
     int est_hidden = 0;
     float *est_w1t = nullptr, *est_b1 = nullptr, *est_w2 = nullptr, *est_b2 = nullptr, *est_pooled = nullptr;
@@ -241,6 +245,11 @@ int upload_fragments(thia_model* m, const HostLayer& a, bf16_t** out) {
     HIP_TRY(m, hipMemcpy(*out, frag.data(), frag.size() * 2, hipMemcpyHostToDevice));
     return THIA_OK;
 }
+void free_head_i8(ExitUnit& E) {
+    thia_linear_i8_free(E.fc1_i8);
+    thia_linear_i8_free(E.fc2_i8);
+    E.fc1_i8 = E.fc2_i8 = nullptr;
+}
 void free_layer(Layer& L) {
     if (L.w) (void)hipFree(L.w);
     if (L.b) (void)hipFree(L.b);
@@ -301,7 +310,7 @@ void free_workspace(thia_model* m) {   // the current lane's
 int ensure_workspace(thia_model* m, int H, int W) {
     const int mb = microbatch_frames(m, H, W);
     Workspace& ws = m->ws;
-    if (ws.arena && ws.H == H && ws.W == W && ws.mb == mb) return THIA_OK;
+    if (ws.arena && ws.H == H && ws.W == W && ws.mb == mb && (ws.codes || m->head_bits != 8)) return THIA_OK;
     if (ws.arena) {
         HIP_TRY(m, hipStreamSynchronize(m->stream));
         free_workspace(m);
@@ -340,6 +349,11 @@ int ensure_workspace(thia_model* m, int H, int W) {
     const size_t o_cs = ap.add(rows * m->Kc * 4), o_cb = ap.add(rows * m->Kc * 16);
     const int key_cap = next_pow2(m->post * m->Kc);
     const size_t o_keys = ap.add((size_t)mb * key_cap * 8);
+    size_t o_codes = 0, o_scales = 0;
+    if (m->head_bits == 8) {
+        o_codes = ap.add(rows * std::max(thia_i8_pitch(m->pool * m->pool * ch_max), thia_i8_pitch(m->fc_dim)));
+        o_scales = ap.add(rows * 4);
+    }
 
     void* base = nullptr;
     hipError_t e = hipMalloc(&base, ap.off);
@@ -360,6 +374,7 @@ int ensure_workspace(thia_model* m, int H, int W) {
     ws.cls = reinterpret_cast<float*>(a + o_cls); ws.box = reinterpret_cast<float*>(a + o_box);
     ws.cand_scores = reinterpret_cast<float*>(a + o_cs); ws.cand_boxes = reinterpret_cast<float*>(a + o_cb);
     ws.sel_keys = reinterpret_cast<uint64_t*>(a + o_keys); ws.key_cap = key_cap;
+    if (m->head_bits == 8) { ws.codes = reinterpret_cast<int8_t*>(a + o_codes); ws.code_scales = reinterpret_cast<float*>(a + o_scales); }
     return THIA_OK;
 }
 
@@ -487,6 +502,14 @@ int run_conv(thia_model* m, int cls, const Layer& L, const void* in, int n, int 
     Scope sc(m, cls);
     HIP_TRY(m, launch_conv(a, m->precision, out_f32, m->stream));
     return THIA_OK;
+}
+
+// A fully connected layer with ReLU in 8 bits: the rows' codes, then the product.
+int run_fc_i8(thia_model* m, const thia_linear_i8* l, const void* in, int rows, int k, void* out) {
+    Scope sc(m, THIA_K_FC);
+    int rc = thia_quantize_rows(in, k, m->precision, rows, k, m->ws.codes, m->ws.code_scales, m->stream);
+    if (rc == THIA_OK) rc = thia_linear_i8_run(l, m->ws.codes, m->ws.code_scales, rows, nullptr, 0, 1, m->precision, out, m->fc_dim, m->stream);
+    return rc == THIA_OK ? rc : fail(m, rc, std::string("8-bit layer: ") + thia_i8_last_error());
 }
 
 int tap_prepare(thia_model* m, int which, int n, size_t per_frame) {
@@ -697,8 +720,13 @@ int run_heads(thia_model* m, const void* feat, int f0, int nb, int H, int W, int
         HIP_TRY(m, launch_roialign(hf, ws.rois, nb, m->post, g.Hk, g.Wk, Ch, g.stride, P, m->precision, ws.roi_feat, m->stream));
     }
     const int rows = nb * m->post;
-    TRY(run_conv(m, THIA_K_FC, E.fc1, ws.roi_feat, rows, 1, 1, 1, 0, nullptr, true, false, ws.h1));
-    TRY(run_conv(m, THIA_K_FC, E.fc2, ws.h1, rows, 1, 1, 1, 0, nullptr, true, false, ws.h2));
+    if (m->head_bits == 8) {
+        TRY(run_fc_i8(m, E.fc1_i8, ws.roi_feat, rows, E.fc1.ci, ws.h1));
+        TRY(run_fc_i8(m, E.fc2_i8, ws.h1, rows, E.fc2.ci, ws.h2));
+    } else {
+        TRY(run_conv(m, THIA_K_FC, E.fc1, ws.roi_feat, rows, 1, 1, 1, 0, nullptr, true, false, ws.h1));
+        TRY(run_conv(m, THIA_K_FC, E.fc2, ws.h1, rows, 1, 1, 1, 0, nullptr, true, false, ws.h2));
+    }
     TRY(run_conv(m, THIA_K_FC, E.pred, ws.h2, rows, 1, 1, 1, 0, nullptr, false, true, ws.cls, ws.box, m->Kc));
     {
         Scope sc(m, THIA_K_POST);
@@ -1163,6 +1191,7 @@ void thia_free_model(thia_model* m) {
         if (E.head_fb) (void)hipFree(E.head_fb);
         if (E.lat_f) (void)hipFree(E.lat_f);
         E.head_f = nullptr; E.head_fb = nullptr; E.lat_f = nullptr;
+        free_head_i8(E);
     }
     delete m;
 }
@@ -1179,6 +1208,27 @@ int thia_set_lanes(thia_model* m, int lanes) {
     if (!m) return THIA_E_BADARG;
     if (lanes < 1 || lanes > 2) return fail(m, THIA_E_BADARG, "lanes must be 1 or 2");
     m->lanes = lanes;
+    return THIA_OK;
+}
+
+int thia_set_head_bits(thia_model* m, int bits) {
+    if (!m) return THIA_E_BADARG;
+    if (bits != 0 && bits != 8) return fail(m, THIA_E_BADARG, "head bits must be 0 (the model's own type) or 8");
+    HIP_TRY(m, hipStreamSynchronize(m->stream));
+    if (m->lane_stream) HIP_TRY(m, hipStreamSynchronize(m->lane_stream));
+    int rc = THIA_OK;
+    for (int e = 0; e < m->n_exits && rc == THIA_OK; ++e) {
+        ExitUnit& E = m->ex[e];
+        if (bits == 0) free_head_i8(E);
+        if (bits == 8 && !E.fc1_i8) rc = linear_i8_from_rows(E.fc1.w, m->precision, E.fc1.b, E.fc1.co, E.fc1.ci, &E.fc1_i8);
+        if (rc == THIA_OK && bits == 8 && !E.fc2_i8) rc = linear_i8_from_rows(E.fc2.w, m->precision, E.fc2.b, E.fc2.co, E.fc2.ci, &E.fc2_i8);
+    }
+    if (rc != THIA_OK) {
+        if (m->head_bits != 8)
+            for (int e = 0; e < m->n_exits; ++e) free_head_i8(m->ex[e]);
+        return fail(m, rc, std::string("8-bit layers: ") + thia_i8_last_error());
+    }
+    m->head_bits = bits;
     return THIA_OK;
 }
 

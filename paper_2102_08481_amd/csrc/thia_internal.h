@@ -217,6 +217,8 @@ hipError_t launch_fill_empty(int n, int D, float* out_boxes, float* out_scores, 
 constexpr int kMaxI8Cols = 65536, kMaxI8Channels = 1 << 20;
 // Keeps `why` (a string that lives on) as this thread's thia_i8_last_error and returns `code`.
 int i8_fail(int code, const char* why);
+// An 8-bit layer from rows of weights [n][k] (fp32 or bf16 per precision) and biases [n] on the device, quantized per row; waits.
+int linear_i8_from_rows(const void* rows, int precision, const float* bias, int n, int k, thia_linear_i8** out);
 
 // ---------------------------------------------------------------- query planning (host logic + the predicate kernel)
 // flags[r] = (number of slots d of row r with labels[r][d] == label and scores[r][d] >= min_score) >= min_count

@@ -340,3 +340,60 @@ def test_block_captured_and_on_other_streams():
             got.append(block(y, r, gain, up, down)[-1])
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+# ---------------------------------------------------------------- the box head in 8 bits
+def head_layers(spec, blob, ep):
+    """Exit ep's wide layers from the blob, in the element type and order the library keeps them, and the predictors in 64 bits."""
+    import paper_2102_08481_amd as thia
+    from thia_synth import split_blob
+    t = {k: torch.from_numpy(v.copy()).cuda() for k, v in split_blob(spec, blob).items() if k.startswith(f"e{ep}.")}
+    dtype = BF if spec.precision else F
+    w1 = t[f"e{ep}.fc1.w"]
+    w1 = w1.reshape(w1.shape[0], -1, 49).transpose(1, 2).reshape(w1.shape[0], -1)   # [c][bin] -> [bin][c]
+    layers = [thia.thia_linear_i8_load(w.to(dtype).float(), t[f"e{ep}.{n}.b"]) for n, w in (("fc1", w1), ("fc2", t[f"e{ep}.fc2.w"]))]
+    return layers, [(t[f"e{ep}.{n}.w"].to(dtype).double(), t[f"e{ep}.{n}.b"].double()) for n in ("cls", "box")]
+
+
+@pytest.mark.parametrize("precision", [1, 0])
+def test_box_head_in_8_bits(precision):
+    """The head's wide layers in 8 bits are the public calls on the same rows, bit for bit; back in the model's type everything is as
+    it was; frames do not depend on their neighbours."""
+    import numpy as np
+    import paper_2102_08481_amd as thia
+    from gpu_common import MINI_BF16, MINI_FP32, biased_model
+    from thia_synth import CONFIGS, make_frames
+    spec = MINI_BF16 if precision else MINI_FP32
+    model, blob = biased_model(spec, 77)
+    frames = torch.from_numpy(np.random.RandomState(5).randint(0, 256, (5, 3, 130, 190)).astype(np.uint8)).cuda()
+    ep = 2
+    before = [v.clone() for v in model.detect_chunk(frames, ep)]
+    try:
+        model.set_head_bits(8)
+        model.set_debug(True)
+        eight = [v.clone() for v in model.detect_chunk(frames, ep)]
+        torch.cuda.synchronize()
+        feat = torch.from_numpy(model.tap("roi_feat")).cuda().to(BF if precision else F).reshape(5 * spec.post_nms, -1)
+        logits, deltas = (torch.from_numpy(model.tap(n)).cuda().double().reshape(5 * spec.post_nms, -1) for n in ("cls_logits", "box_deltas"))
+        model.set_debug(False)
+        (fc1, fc2), preds = head_layers(spec, blob, ep)
+        h1 = thia.thia_linear_i8_run(fc1, *thia.thia_quantize_rows(feat), relu=True, out_f32=not precision)
+        h2 = thia.thia_linear_i8_run(fc2, *thia.thia_quantize_rows(h1), relu=True, out_f32=not precision).double()
+        for got, (w, b) in zip((logits, deltas), preds):
+            # products of the same elements added in fp32, `fc_dim` of them and the bias, each addition off by at most 1 u of the sum of sizes
+            size = h2.abs() @ w.abs().t().contiguous() + b.abs()
+            assert ((got - (h2 @ w.t().contiguous() + b)).abs() <= (spec.fc_dim + 2) * U * size).all()
+        for i in range(5):
+            alone = model.detect_chunk(frames[i:i + 1].contiguous(), ep)
+            assert all(torch.equal(a[0], b[i]) for a, b in zip(alone, eight))
+        chunks = model.run_chunks(frames, [(0, 2, ep), (2, 3, ep)])
+        assert all(torch.equal(a, b) for a, b in zip(chunks, eight))
+        every = model.detect_all_exits(frames)
+        assert all(torch.equal(a[ep - 1], b) for a, b in zip(every, eight))
+        with pytest.raises(thia.ThiaError):
+            model.set_head_bits(4)
+    finally:
+        model.set_debug(False)
+        model.set_head_bits(0)
+    assert all(torch.equal(a, b) for a, b in zip(before, model.detect_chunk(frames, ep)))
+    assert not torch.equal(before[1], eight[1])   # the option does something
