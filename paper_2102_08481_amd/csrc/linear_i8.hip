@@ -152,15 +152,24 @@ __device__ inline void finish_rows(const LinearArgs& a, const i32x16_t (&acc)[2]
 #include "linear_i8_small.h"
 #include "linear_i8_tiny.h"
 
-// Which tile: the one with the least base + rounds * K tiles * per_k + max(1, tiles / 256) * per_tile, in us, `rounds` the tiles that one
-// of the 256 CUs gets (ceil).  The constants are a least-squares fit (relative errors) to 120 shapes of 1 to 16 384 rows, 128 to 12 544
-// columns and 64 to 8 192 channels; over these the rule is 0.7 % from the best of the seven in the geometric mean, 22 % at worst (a call of 3 us).
-// us, 16 x 16 / 32 x 32 / 32 x 64 / 64 x 64 / 128 x 128 / 192 x 256 / 256 x 256 (rows x columns x channels): 1 x 4096 x 4096 3.9 / 4.7 / 5.5 / 7.0 / - / - / -;
-// 130 x 4096 x 512 7.5 / 4.8 / 5.9 / 7.9 / 19 / 31 / 38; 700 x 256 x 2048 9.0 / 6.3 / 4.9 / 5.6 / 7.9 / 10.1 / 12.1; 1000 x 12544 x 1024 - / 57 / - / 24 / 46 / 78 / 94;
-// 4000 x 1024 x 1024 - / 21 / 15.6 / 15.1 / 11.7 / 15.5 / 18.2; 9600 x 12544 x 1024 128 x 128 165, 107 / 117; 8192 x 8192 x 8192 707, 502 / 445.
-struct Tile { int rows, chans; double base, per_k, per_tile; };
-constexpr Tile kTiles[] = {{16, 16, 2.66, 0.070, 0.186}, {32, 32, 2.54, 0.063, 0.566}, {32, 64, 2.60, 0.088, 0.784}, {64, 64, 2.39, 0.118, 1.806},
-                           {128, 128, 0.0, 0.452, 6.995}, {192, 256, 0.0, 0.743, 9.045}, {256, 256, 0.0, 0.947, 10.537}};
+// Which tile: the one with the least base + K tiles * (per_k * rounds + more_k * (r - 1)) + per_tile * r, in us, where r is the number of tiles
+// per CU, at least 1, and `rounds` that number rounded up.  The constants are a least-squares fit (relative errors) to what the tiles took on
+// 240 shapes of 1 to 16 384 rows, 128 to 12 544 columns and 64 to 8 192 channels; over these the rule is 2 % from the best tile in the geometric
+// mean, and 30 % at worst.  Measured in us, rows x columns x channels:
+//                        16x16  32x32  32x64  64x64  96x64  128x64  128x128  192x256  256x256
+//   1 x 4096 x 4096        3.9    4.7    5.5    7.0
+//   130 x 4096 x 512       7.5    4.8    5.9    7.9                       19       31       38
+//   700 x 256 x 2048       9.0    6.3    4.9    5.6                      7.9       10       12
+//   700 x 12544 x 1024             34     29     21     26      31        46       77       95
+//   1200 x 12544 x 1024                   46     39     28      32        46       78       96
+//   2000 x 12544 x 1024                   64     60     58      39        47       78       96
+//   4000 x 1024 x 1024             21     16     15     18      18        11       15       18
+//   9600 x 12544 x 1024                                                  165      107      117
+//   8192 x 8192 x 8192                                                   707      502      445
+struct Tile { int rows, chans; double base, per_k, per_tile, more_k; };
+constexpr Tile kTiles[] = {{16, 16, 2.80, 0.064, 0.081, 0.037},  {32, 32, 2.66, 0.060, 0.507, 0.020},   {32, 64, 2.85, 0.089, 0.590, 0.044},
+                           {64, 64, 2.68, 0.144, 1.527, 0.064},  {96, 64, 0.03, 0.230, 4.708, 0.0},     {128, 64, 1.12, 0.288, 5.238, 0.050},
+                           {128, 128, 0.0, 0.453, 7.392, 0.128}, {192, 256, 0.0, 0.828, 9.825, 0.792}, {256, 256, 0.0, 1.066, 11.711, 0.927}};
 
 int choose_tile(int rows, int n, int pitch) {
     int best = 0;
@@ -169,9 +178,10 @@ int choose_tile(int rows, int n, int pitch) {
         const Tile& t = kTiles[i];
         if (t.chans == 256 && pitch < 256) continue;   // two K tiles are under way there
         const double tiles = (double)((rows + (long long)t.rows - 1) / t.rows) * ((n + t.chans - 1) / t.chans);
-        double per_k = t.per_k;
-        if (i == 0) per_k *= 0.5 + 0.03125 * (rows < 16 ? rows : 16);   // rows that do not exist are not fetched
-        const double us = t.base + ceil(tiles / 256) * (pitch / 128) * per_k + (tiles > 256 ? tiles / 256 : 1.0) * t.per_tile;
+        const double r = tiles > 256 ? tiles / 256 : 1.0;
+        double k_tiles = pitch / 128;
+        if (t.rows == 16) k_tiles *= 0.5 + 0.03125 * (rows < 16 ? rows : 16);   // rows that do not exist are not fetched
+        const double us = t.base + k_tiles * (t.per_k * ceil(tiles / 256) + t.more_k * (r - 1)) + t.per_tile * r;
         if (i == 0 || us < least) { best = i; least = us; }
     }
     return best;
@@ -184,8 +194,10 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t s) {
         case 1: return launch_small<T, 1, 1, 4, 2>(a, s);
         case 2: return launch_small<T, 1, 2, 4, 1>(a, s);
         case 3: return launch_small<T, 2, 2, 4, 1>(a, s);
-        case 4: return launch_mid<T, 128, 128, 4>(a, s);
-        case 5: return launch_large<T, 192>(a, s);
+        case 4: return launch_small<T, 3, 2, 4, 1>(a, s);
+        case 5: return launch_small<T, 4, 2, 4, 1>(a, s);
+        case 6: return launch_mid<T, 128, 128, 4>(a, s);
+        case 7: return launch_large<T, 192>(a, s);
         default: return launch_large<T, 256>(a, s);
     }
 }
