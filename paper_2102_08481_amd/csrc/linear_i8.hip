@@ -57,8 +57,16 @@ __device__ inline __amdgpu_buffer_rsrc_t buffer(const void* p, uint32_t bytes) {
 __device__ inline i32x16_t mma_i8(const u32x4_t& w, const u32x4_t& x, const i32x16_t& acc) {
     return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4_t, w), __builtin_bit_cast(i32x4_t, x), acc, 0, 0, 0);
 }
-// ReLU that keeps a NaN.
-__device__ inline float relu_if(bool relu, float v) { return relu && v < 0.f ? 0.f : v; }
+// The sum of channel c in fp32: every tile rounds alike, so that a row's result does not depend on the tile.
+__device__ inline float scaled(int sum, float xs, float ws, float b) { return __builtin_fmaf((float)sum * xs, ws, b); }
+// ReLU that keeps a NaN, on N values.
+template <int N>
+__device__ inline void relu_if(int relu, float (&v)[N]) {
+    if (relu) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];
+    }
+}
 
 // ---- epilogue of the smaller tiles: four channels from ch (a multiple of 4) on of row m, if it exists.
 template <typename T>
@@ -68,7 +76,7 @@ __device__ inline void finish_four(const LinearArgs& a, const i32x4_t& s, size_t
     const f32x4_t ws = *reinterpret_cast<const f32x4_t*>(a.wscale + ch), b = *reinterpret_cast<const f32x4_t*>(a.bias + ch);
     float v[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = ((float)s[e] * xs) * ws[e] + b[e];
+    for (int e = 0; e < 4; ++e) v[e] = scaled(s[e], xs, ws[e], b[e]);
     T* out = static_cast<T*>(a.out) + m * a.ldo + ch;
     const T* res = a.res ? static_cast<const T*>(a.res) + m * a.ldr + ch : nullptr;
     if (a.vec) {
@@ -78,13 +86,18 @@ __device__ inline void finish_four(const LinearArgs& a, const i32x4_t& s, size_t
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] += r[e];
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = relu_if(a.relu, v[e]);
+        relu_if(a.relu, v);
         store4(out, v);
     } else {
+        if (res) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (ch + e < a.n) v[e] += load_elem(res + e);
+        }
+        relu_if(a.relu, v);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (ch + e < a.n) store_elem(out + e, relu_if(a.relu, v[e] + (res ? load_elem(res + e) : 0.f)));
+            if (ch + e < a.n) store_elem(out + e, v[e]);
     }
 }
 
@@ -108,6 +121,9 @@ __device__ inline void finish_rows(const LinearArgs& a, const i32x16_t (&acc)[2]
     constexpr bool AHEAD = sizeof(T) == 2;
     Vec8<T> next[4], now[4];
     const bool ahead = AHEAD && a.vec && a.res;
+    // bf16 without a residual: rounded in front of LDS, which then takes half the bytes
+    constexpr int ROUNDED_PITCH = 64 * 2 + 16;
+    const bool rounded = sizeof(T) == 2 && a.vec && !a.res;
     auto fetch = [&](int j) {
 #pragma unroll
         for (int it = 0; it < 4; ++it) {
@@ -129,14 +145,27 @@ __device__ inline void finish_rows(const LinearArgs& a, const i32x16_t (&acc)[2]
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                f32x4_t r;
+                float r[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) r[e] = ((float)acc[i][j][4 * v + e] * xs) * ws[i][v][e] + bs[i][v][e];
-                *reinterpret_cast<f32x4_t*>(ep + (size_t)frag_row * FINISH_PITCH + (i * 32 + 8 * v + 4 * (lane >> 5)) * 4) = r;
+                for (int e = 0; e < 4; ++e) r[e] = scaled(acc[i][j][4 * v + e], xs, ws[i][v][e], bs[i][v][e]);
+                const int ch = i * 32 + 8 * v + 4 * (lane >> 5);
+                if (rounded) {
+                    relu_if(a.relu, r);
+                    *reinterpret_cast<u32x2_t*>(ep + (size_t)frag_row * ROUNDED_PITCH + ch * 2) = u32x2_t{pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3])};
+                } else {
+                    store4(reinterpret_cast<float*>(ep + (size_t)frag_row * FINISH_PITCH + ch * 4), r);
+                }
             }
         __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the region is private to this wavefront
         __builtin_amdgcn_wave_barrier();
-        if (a.vec) {
+        if (rounded) {
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                const int r = it * 8 + (lane >> 3), c = (lane & 7) * 8;
+                if (rj + r < rows && nw + c < a.n)
+                    *reinterpret_cast<u32x4_t*>(static_cast<T*>(a.out) + (m0 + rj + r) * a.ldo + nw + c) = *reinterpret_cast<const u32x4_t*>(ep + (size_t)r * ROUNDED_PITCH + c * 2);
+            }
+        } else if (a.vec) {
 #pragma unroll
             for (int it = 0; it < 4; ++it) {   // eight lanes per row
                 const int r = it * 8 + (lane >> 3), c = (lane & 7) * 8;
@@ -148,16 +177,16 @@ __device__ inline void finish_rows(const LinearArgs& a, const i32x16_t (&acc)[2]
 #pragma unroll
                     for (int e = 0; e < 8; ++e) o[e] += y[e];
                 }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = relu_if(a.relu, o[e]);
+                relu_if(a.relu, o);
                 store8(static_cast<T*>(a.out) + (m0 + rj + r) * a.ldo + nw + c, o);
             }
         } else if (nw + lane < a.n) {
             for (int r = 0; r < 32 && rj + r < rows; ++r) {
                 const size_t m = m0 + rj + r;
-                float o = *reinterpret_cast<const float*>(ep + (size_t)r * FINISH_PITCH + lane * 4);
-                if (a.res) o += load_elem(static_cast<const T*>(a.res) + m * a.ldr + nw + lane);
-                store_elem(static_cast<T*>(a.out) + m * a.ldo + nw + lane, relu_if(a.relu, o));
+                float o[1] = {*reinterpret_cast<const float*>(ep + (size_t)r * FINISH_PITCH + lane * 4)};
+                if (a.res) o[0] += load_elem(static_cast<const T*>(a.res) + m * a.ldr + nw + lane);
+                relu_if(a.relu, o);
+                store_elem(static_cast<T*>(a.out) + m * a.ldo + nw + lane, o[0]);
             }
         }
         __builtin_amdgcn_s_waitcnt(0xc07f);
