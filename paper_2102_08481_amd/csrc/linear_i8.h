@@ -5,6 +5,9 @@
 // Weights lie in matrix-instruction fragments: for every 32 channels and 32 k one contiguous 1 KiB in which lane l's 16 bytes are
 // v[32 ct + l % 32][32 ks + 16 (l / 32) .. + 15]; rows and k behind the last are zeros, so what an activation row holds behind
 // column k does not matter.
+//
+// Part of roi.hip, which includes it once, at its end.
+#pragma once
 #include <math.h>
 
 #include <new>

@@ -15,7 +15,7 @@
 // memory part.  A half that phase j reads has landed for all wavefronts when phase j starts: each waits in phase j - 1, in front of its
 // barrier, until no more of its requests are outstanding than it issued behind that half (vmcnt counts them in order).
 //
-// Part of linear_i8.hip, which includes it once.
+// Part of linear_i8.h, which includes it once.
 template <typename T, int BM>
 __global__ __launch_bounds__(512, 1) void linear_large_kernel(const LinearArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)

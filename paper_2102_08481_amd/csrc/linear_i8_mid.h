@@ -2,7 +2,7 @@
 // into a ring of R in LDS, R - 1 on their way; one barrier per K tile hands the next one over and gives the last one's place back.
 // Fragments of the next K tile are read between the products of this one.
 //
-// Part of linear_i8.hip, which includes it once.
+// Part of linear_i8.h, which includes it once.
 template <typename T, int BM, int BN, int R>
 __global__ __launch_bounds__(BM * BN / 64) void linear_mid_kernel(const LinearArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)

@@ -1,7 +1,7 @@
 // Few rows or few tiles: 32 TM rows x 32 TN channels per block of W wavefronts that share the contraction: wavefront w takes the 128-byte
 // pieces w, w + W, ... of every row, with D pieces on their way while one is multiplied, and waits for no other wavefront.  The W partial sums meet in LDS (whole numbers: their order does not matter).
 //
-// Part of linear_i8.hip, which includes it once.
+// Part of linear_i8.h, which includes it once.
 //
 // LDS of a wavefront: D + 1 pieces of its rows, and later its sums.
 constexpr int small_region(int tm, int tn, int d) { return (d + 1) * tm * 4096 > tm * tn * 8 * 33 * 16 ? (d + 1) * tm * 4096 : tm * tn * 8 * 33 * 16; }

@@ -3,7 +3,7 @@
 // is the fastest although it fetches the most.  Both operands come straight from memory, lane l taking row l % 16 and the 16-byte
 // chunk l / 16 of 64 k: 64 bytes of each of 16 rows, of the weights four runs of 256 bytes.
 //
-// Part of linear_i8.hip, which includes it once.
+// Part of linear_i8.h, which includes it once.
 template <typename T, int W>
 __global__ __launch_bounds__(64 * W) void linear_tiny_kernel(const LinearArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)

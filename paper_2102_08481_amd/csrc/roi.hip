@@ -1,6 +1,6 @@
 // ROI head kernels: ROIAlign gather on the NHWC head feature map, class scores and
 // per-class box decoding, and the final detection selection (threshold, ordering,
-// same-class greedy NMS, top-D).
+// same-class greedy NMS, top-D).  Included at the end: rows and products in 8 bits.
 #include "device_util.h"
 
 #include <type_traits>
@@ -559,3 +559,7 @@ hipError_t launch_fill_empty(int n, int D, float* out_boxes, float* out_scores, 
 }
 
 }  // namespace thia
+
+// The box head's wide layers in 8 bits, and the public calls they are made of.
+#include "rows_i8.h"
+#include "linear_i8.h"

@@ -1,9 +1,12 @@
-// Rows in 8 bits: what stands in front of a product of 8-bit integers (linear_i8.hip).  A row y becomes whole numbers q in
+// Rows in 8 bits: what stands in front of a product of 8-bit integers (linear_i8.h).  A row y becomes whole numbers q in
 // -127..127 and one scale s with y = q s:
 //   quantize:  s = max|y| / 127, q = y / s rounded to nearest even.
 //   norm:      h = x (+ r), y = h g / sqrt(mean(h^2) + eps), then the same.  q depends on y's direction alone, so it is h g 127 / max|h g|
 //              whatever the norm is, and one reduction of a row (sum h^2 and max|h g|) gives both the codes and the scale
 //              max|h g| / (127 sqrt(mean + eps)).
+//
+// Part of roi.hip, which includes it once, at its end.
+#pragma once
 #include "conv_common.h"
 
 namespace thia {
