@@ -319,8 +319,15 @@ extern "C" {
 
 void thia_linear_i8_free(thia_linear_i8* l) {
     if (!l) return;
-    if (l->w) (void)hipFree(l->w);
-    if (l->scale_bias) (void)hipFree(l->scale_bias);
+    if (l->w || l->scale_bias) {
+        int dev = l->device;
+        (void)hipGetDevice(&dev);
+        if (dev != l->device) (void)hipSetDevice(l->device);
+        (void)hipDeviceSynchronize();   // calls that read them may be under way on any stream
+        if (l->w) (void)hipFree(l->w);
+        if (l->scale_bias) (void)hipFree(l->scale_bias);
+        if (dev != l->device) (void)hipSetDevice(dev);
+    }
     delete l;
 }
 
@@ -358,6 +365,7 @@ int thia_linear_i8_run(const thia_linear_i8* l, const int8_t* codes, const float
     if (!l || rows < 0 || (rows > 0 && (!codes || !scales || !out))) return i8_fail(THIA_E_BADARG, "null pointer or negative row count");
     if (precision != 0 && precision != 1) return i8_fail(THIA_E_BADARG, "precision must be 0 (fp32) or 1 (bf16)");
     if (ldo < l->n || (residual && ldr < l->n)) return i8_fail(THIA_E_BADARG, "row pitch smaller than the row");
+    if (residual && residual == out && rows > 1 && ldr != ldo) return i8_fail(THIA_E_BADARG, "a result in place of the residual needs its pitch");
     const uintptr_t elem = precision ? 2 : 4;
     if ((uintptr_t)codes % 16 || (uintptr_t)scales % 4 || (uintptr_t)out % elem || (uintptr_t)residual % elem)
         return i8_fail(THIA_E_BADARG, "misaligned pointer (codes: 16 bytes, others: their element)");

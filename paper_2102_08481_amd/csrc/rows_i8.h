@@ -271,6 +271,7 @@ int thia_rms_norm_i8(const void* x, long long ldx, const void* residual, long lo
     if (!(eps > 0.f) || !(eps <= 3.4028235e38f)) return i8_fail(THIA_E_BADARG, "eps must be positive and finite");
     if (sum && !residual) return i8_fail(THIA_E_BADARG, "a sum without a residual");
     if ((residual && ldr < k) || (sum && ldsum < k)) return i8_fail(THIA_E_BADARG, "row pitch smaller than the row");
+    if (sum && rows > 1 && ((sum == x && ldsum != ldx) || (sum == residual && ldsum != ldr))) return i8_fail(THIA_E_BADARG, "a sum in place of an input needs its pitch");
     const uintptr_t elem = precision ? 2 : 4;
     if ((uintptr_t)residual % elem || (uintptr_t)sum % elem || (uintptr_t)gain % 4) return i8_fail(THIA_E_BADARG, "misaligned pointer");
     if (k > kMaxI8Cols) return i8_fail(THIA_E_SHAPE, "more than 65536 columns");

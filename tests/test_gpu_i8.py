@@ -190,6 +190,74 @@ def test_linear(rows, k, n, dtype):
     check_product(thia.thia_linear_i8_run(layer, codes, scales, True, residual, dtype is F), codes, scales, w, ws, b, k, True, residual)
 
 
+# ragged shapes that reach every tile: 16 x 16, 32 x 32, 32 x 64, 64 x 64, 96 x 64, 128 x 64, 128 x 128, 192 x 256, 256 x 256, the rings and
+# phases with two, three and more K tiles
+RAGGED = [(5, 200, 37), (700, 640, 130), (1003, 2000, 515), (2001, 1000, 1001), (1187, 12001, 1003), (2003, 12544, 1000), (2100, 100, 1999), (2001, 200, 1999),
+          (3000, 257, 1030), (9001, 130, 1001), (2901, 300, 2001), (4001, 700, 4099), (4097, 200, 4090), (4001, 300, 4001), (8190, 400, 4104)]
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("rows,k,n", RAGGED)
+def test_linear_ragged(rows, k, n, dtype):
+    """Every tile with rows and channels that end inside it: dense and pitched results, with and without a residual, nothing written
+    beside them."""
+    import paper_2102_08481_amd as thia
+    layer, w, ws, b = layer_of(rows + n, n, k)
+    codes, scales = codes_of(k, rows, k)
+    out = thia.thia_linear_i8_run(layer, codes, scales, True, out_f32=dtype is F)
+    check_product(out, codes, scales, w, ws, b, k, True)
+    res = rows_of(9, rows, n + 3, dtype)[:, 1:n + 1]
+    want = thia.thia_linear_i8_run(layer, codes, scales, False, res.contiguous(), dtype is F)
+    check_product(want, codes, scales, w, ws, b, k, False, res)
+    room = torch.full((rows + 2, n + 7), 7, dtype=dtype, device="cuda")
+    thia.thia_linear_i8_run(layer, codes, scales, False, res, dtype is F, out=room[:rows, 3:n + 3])
+    assert torch.equal(room[:rows, 3:n + 3], want)
+    room[:rows, 3:n + 3] = 7
+    assert (room == 7).all()
+    inplace = res.contiguous()
+    thia.thia_linear_i8_run(layer, codes, scales, False, inplace, dtype is F, out=inplace)
+    assert torch.equal(inplace, want)
+
+
+def test_more_rows_than_one_launch_holds():
+    import paper_2102_08481_amd as thia
+    layer, w, ws, b = layer_of(3, 3, 5)
+    codes, scales = codes_of(4, 1600003, 5)
+    check_product(thia.thia_linear_i8_run(layer, codes, scales, out_f32=True), codes, scales, w, ws, b, 5)
+    x = codes[:, :5].float()
+    check_codes(*thia.thia_quantize_rows(x), x.double(), 5, 2)
+
+
+@pytest.mark.parametrize("rows,k", [(33003, 65536), (270001, 8000)])
+def test_offsets_beyond_32_bits(rows, k):
+    """Inputs, codes and results of more than 2^31 bytes: the last rows are those of the same rows alone."""
+    import paper_2102_08481_amd as thia
+    x = torch.empty((rows, k), dtype=BF, device="cuda")
+    x[-40:] = rows_of(1, 40, k, BF)
+    x[:-40] = 1
+    r = torch.zeros_like(x)
+    r[-40:] = rows_of(2, 40, k, BF)
+    gain = 0.5 + torch.rand(k, device="cuda")
+    codes, scales = thia.thia_quantize_rows(x)
+    want = thia.thia_quantize_rows(x[-40:].contiguous())
+    assert torch.equal(codes[-40:], want[0]) and torch.equal(scales[-40:], want[1])
+    layer, *_ = layer_of(3, 40, k)
+    assert torch.equal(thia.thia_linear_i8_run(layer, codes, scales)[-40:], thia.thia_linear_i8_run(layer, *want))
+    codes, scales, total = thia.thia_rms_norm_i8(x, gain, 1e-6, r)
+    want = thia.thia_rms_norm_i8(x[-40:].contiguous(), gain, 1e-6, r[-40:].contiguous())
+    assert all(torch.equal(a[-40:], b) for a, b in zip((codes, scales, total), want))
+
+
+@pytest.mark.parametrize("n,out_f32", [(30007, True), (60000, False)])
+def test_results_beyond_32_bits(n, out_f32):
+    import paper_2102_08481_amd as thia
+    layer, *_ = layer_of(1, n, 300)
+    codes, scales = codes_of(2, 40003, 300)
+    res = torch.ones((40003, n), dtype=F if out_f32 else BF, device="cuda")
+    out = thia.thia_linear_i8_run(layer, codes, scales, False, res, out_f32)
+    assert torch.equal(out[-70:], thia.thia_linear_i8_run(layer, codes[-70:], scales[-70:], False, res[-70:], out_f32))
+
+
 @pytest.mark.parametrize("rows", [1, 20, 700, 4000])
 def test_the_largest_sums(rows):
     """65536 products of -128 and -128: 2^30; and the layer takes -128 on both sides."""

@@ -43,7 +43,7 @@ def test_quantize_refuses(L, change, code):
 @pytest.mark.parametrize("change,code", [
     (dict(x=None), BADARG), (dict(gain=None), BADARG), (dict(codes=None), BADARG), (dict(scales=None), BADARG), (dict(rows=-1), BADARG), (dict(k=0), BADARG),
     (dict(eps=0.0), BADARG), (dict(eps=-1.0), BADARG), (dict(eps=float("nan")), BADARG), (dict(eps=float("inf")), BADARG), (dict(r=None), BADARG),
-    (dict(ldx=7), BADARG), (dict(ldr=7), BADARG), (dict(ldsum=7), BADARG), (dict(r=A + 1), BADARG), (dict(sum=A + 1), BADARG), (dict(gain=A + 2), BADARG),
+    (dict(ldx=7), BADARG), (dict(ldr=7), BADARG), (dict(ldsum=7), BADARG), (dict(ldsum=9), BADARG), (dict(sum=A + 64, r=A + 64, ldr=9), BADARG), (dict(r=A + 1), BADARG), (dict(sum=A + 1), BADARG), (dict(gain=A + 2), BADARG),
     (dict(precision=2), BADARG), (dict(k=65537, ldx=65537, ldr=65537, ldsum=65537), SHAPE)])
 def test_norm_refuses(L, change, code):
     assert L.thia_rms_norm_i8(*{**NORM, **change}.values()) == code
