@@ -2,6 +2,11 @@
 // into a ring of R in LDS, R - 1 on their way; one barrier per K tile hands the next one over and gives the last one's place back.
 // Fragments of the next K tile are read between the products of this one.
 //
+// A K tile of a 128 x 128 block is 512 cycles of products per SIMD, 64 KB of fragment reads and 32 KB of requests (768 cycles of LDS).
+// 4096 x 4096 x 1024 (256 blocks) takes 23.3 us; without its requests it was 21, without fragment reads as well 19.5, of which about 5
+// are launch, first operands and results: products at the clock that the chip keeps under matrix work are most of it.  Requests
+// issued together in front of the products held up everything behind them (900 x 12544 x 1024 52 us, between the products 46).
+//
 // Part of linear_i8.h, which includes it once.
 template <typename T, int BM, int BN, int R>
 __global__ __launch_bounds__(BM * BN / 64) void linear_mid_kernel(const LinearArgs a) {

@@ -4,6 +4,11 @@
 //   norm:      h = x (+ r), y = h g / sqrt(mean(h^2) + eps), then the same.  q depends on y's direction alone, so it is h g 127 / max|h g|
 //              whatever the norm is, and one reduction of a row (sum h^2 and max|h g|) gives both the codes and the scale
 //              max|h g| / (127 sqrt(mean + eps)).
+// What bounds them is memory: a row is read once and lies in registers until its codes are written.  us and TB/s (a copy of 1 GiB: 4.97): norm
+// with residual and sum 9 600 x 1 024 12.9 / 5.3, 8 192 x 8 192 91 / 5.1, 16 384 x 2 048 37 / 6.3 (the caches hold part of it); codes alone
+// 16 384 x 1 024 9.3 / 5.4, 9 600 x 12 544 93 / 3.9.  Codes written past the caches were quicker by themselves (75 us at 9 600 x 12 544), but not
+// together with the product that reads them (200 us either way); inputs read past them help beyond the caches' size (81 us at 8 192 x 8 192) and cost
+// 15 % below; the next row requested ahead cost occupancy (142 us).
 //
 // Part of roi.hip, which includes it once, at its end.
 #pragma once
