@@ -118,4 +118,23 @@ __device__ inline bool iou_over(const Box& a, const Box& b, float thr) {
     return uni > 0.f && inter > t;
 }
 
+// ---- rows in 8 bits: scale and codes of a row from the bits of its largest size (infinity and NaN sort last)
+__device__ inline uint32_t size_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+__device__ inline float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+// codes are v p0 p1 inv, rounded to nearest even; p0 p1 brings the largest value of a row that leaves the plain range to 1..2
+struct RowScale { float scale, inv, p0, p1; bool ok; };
+__device__ inline RowScale row_scale(uint32_t most) {
+    const float top = __uint_as_float(most);
+    if (top >= 1e-30f && top <= 1e30f) return {top / 127.f, 127.f / top, 1.f, 1.f, true};
+    RowScale r = {__uint_as_float(0x7fc00000u), 0.f, 1.f, 1.f, most < 0x7f800000u};
+    if (!r.ok) return r;
+    const int e = most ? -ilogbf(top) : 0;
+    r.p0 = pow2(e / 2);
+    r.p1 = pow2(e - e / 2);
+    r.scale = (float)((double)top / 127.0);
+    r.inv = most ? 127.f / (top * r.p0 * r.p1) : 0.f;
+    return r;
+}
+__device__ inline uint32_t row_code(const RowScale& r, float v) { return r.ok ? (uint32_t)(int)rintf(v * r.p0 * r.p1 * r.inv) & 255u : 0u; }
+
 }  // namespace thia

@@ -504,10 +504,10 @@ int run_conv(thia_model* m, int cls, const Layer& L, const void* in, int n, int 
     return THIA_OK;
 }
 
-// A fully connected layer with ReLU in 8 bits: the rows' codes, then the product.
+// A fully connected layer with ReLU in 8 bits: the rows' codes (in null: they are in the workspace), then the product.
 int run_fc_i8(thia_model* m, const thia_linear_i8* l, const void* in, int rows, int k, void* out) {
     Scope sc(m, THIA_K_FC);
-    int rc = thia_quantize_rows(in, k, m->precision, rows, k, m->ws.codes, m->ws.code_scales, m->stream);
+    int rc = in ? thia_quantize_rows(in, k, m->precision, rows, k, m->ws.codes, m->ws.code_scales, m->stream) : THIA_OK;
     if (rc == THIA_OK) rc = thia_linear_i8_run(l, m->ws.codes, m->ws.code_scales, rows, nullptr, 0, 1, m->precision, out, m->fc_dim, m->stream);
     return rc == THIA_OK ? rc : fail(m, rc, std::string("8-bit layer: ") + thia_i8_last_error());
 }
@@ -715,13 +715,18 @@ int run_heads(thia_model* m, const void* feat, int f0, int nb, int H, int W, int
         HIP_TRY(m, launch_nms(ws.prop_boxes, ws.prop_n, nb, m->pre, m->rpn_thr, m->post, ws.mask, ws.keep, ws.roi_n, ws.rois,
                               m->stream));
     }
+    // (with taps on, the features themselves are wanted)
+    const bool roi_codes = m->head_bits == 8 && !m->debug && roialign_codes_pay(nb, m->post, Ch, P, m->precision);
     {
         Scope sc(m, THIA_K_ROIALIGN);
-        HIP_TRY(m, launch_roialign(hf, ws.rois, nb, m->post, g.Hk, g.Wk, Ch, g.stride, P, m->precision, ws.roi_feat, m->stream));
+        if (roi_codes)
+            HIP_TRY(m, launch_roialign_codes(hf, ws.rois, nb, m->post, g.Hk, g.Wk, Ch, g.stride, P, m->precision, ws.codes, ws.code_scales, m->stream));
+        else
+            HIP_TRY(m, launch_roialign(hf, ws.rois, nb, m->post, g.Hk, g.Wk, Ch, g.stride, P, m->precision, ws.roi_feat, m->stream));
     }
     const int rows = nb * m->post;
     if (m->head_bits == 8) {
-        TRY(run_fc_i8(m, E.fc1_i8, ws.roi_feat, rows, E.fc1.ci, ws.h1));
+        TRY(run_fc_i8(m, E.fc1_i8, roi_codes ? nullptr : ws.roi_feat, rows, E.fc1.ci, ws.h1));
         TRY(run_fc_i8(m, E.fc2_i8, ws.h1, rows, E.fc2.ci, ws.h2));
     } else {
         TRY(run_conv(m, THIA_K_FC, E.fc1, ws.roi_feat, rows, 1, 1, 1, 0, nullptr, true, false, ws.h1));

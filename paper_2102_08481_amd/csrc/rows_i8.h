@@ -6,13 +6,15 @@
 //              max|h g| / (127 sqrt(mean + eps)).
 // What bounds them is memory: a row is read once and lies in registers until its codes are written.  us and TB/s (a copy of 1 GiB: 4.97): norm
 // with residual and sum 9 600 x 1 024 12.9 / 5.3, 8 192 x 8 192 91 / 5.1, 16 384 x 2 048 37 / 6.3 (the caches hold part of it); codes alone
-// 16 384 x 1 024 9.3 / 5.4, 9 600 x 12 544 93 / 3.9.  Codes written past the caches were quicker by themselves (75 us at 9 600 x 12 544), but not
-// together with the product that reads them (200 us either way); inputs read past them help beyond the caches' size (81 us at 8 192 x 8 192) and cost
-// 15 % below; the next row requested ahead cost occupancy (142 us).
+// 16 384 x 1 024 9.6 / 5.3, 8 192 x 8 192 33 / 6.1, 9 600 x 12 544 74 / 4.9, 1 024 x 65 536 45 / 4.5.  The norm of rows beyond 32 768 columns is the
+// exception (1 024 x 65 536 243 / 1.9): eight values times eight per lane of sixteen wavefronts do not fit their registers beside the residual.
+// Codes written past the caches gained nothing together with the product that reads them (200 us either way for 9 600 x 12 544 x 1024); inputs
+// read past them help beyond the caches' size (norm of 8 192 x 8 192 81 us) and cost 15 % below; the next row requested ahead cost occupancy.
 //
 // Part of roi.hip, which includes it once, at its end.
 #pragma once
 #include "conv_common.h"
+#include "device_util.h"
 
 namespace thia {
 
@@ -53,9 +55,6 @@ __device__ inline void row_store(T* p, int n, const float v[8]) {
     for (int j = 0; j < 8; ++j)
         if (j < n) store_elem(p + j, v[j]);
 }
-
-__device__ inline float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
-__device__ inline uint32_t size_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }   // orders |v|, infinity and NaN last
 
 struct RowStat { float ss; uint32_t most; };   // sum of squares, bits of the largest size
 
@@ -161,50 +160,50 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void rows_i8_kernel(cons
             return reduce(s);
         };
         RowStat s = stat();
-        float scale;
-        bool ok = true;
-        const float most = __uint_as_float(s.most);
-        if (most >= 1e-30f && most <= 1e30f && (!NORM || (s.ss >= 1e-20f && s.ss <= 1e30f))) {
-            scale = most / 127.f;
-            if constexpr (NORM) scale /= sqrtf(s.ss / (float)k + a.eps);
+        RowScale q;
+        if constexpr (!NORM) {
+            q = row_scale(s.most);
         } else {
-            // rows of zeros, of values whose squares or quotients leave fp32, or with a NaN: the row's largest value is brought to 1..2
-            RowStat m = {0.f, 0u};
+            const float most = __uint_as_float(s.most);
+            if (most >= 1e-30f && most <= 1e30f && s.ss >= 1e-20f && s.ss <= 1e30f) {
+                q = {most / 127.f / sqrtf(s.ss / (float)k + a.eps), 127.f / most, 1.f, 1.f, true};
+            } else {
+                // rows of zeros, of values whose squares or quotients leave fp32, or with a NaN: the row's largest value is brought to 1..2
+                RowStat m = {0.f, 0u};
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+                for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t b = size_bits(h[c][j]);
-                    m.most = b > m.most ? b : m.most;
-                }
-            m = reduce(m);
-            ok = m.most < 0x7f800000u;
-            const int e = ok && m.most ? -ilogbf(__uint_as_float(m.most)) : 0;
-            const float p0 = pow2(e / 2), p1 = pow2(e - e / 2);
+                    for (int j = 0; j < 8; ++j) {
+                        const uint32_t b = size_bits(h[c][j]);
+                        m.most = b > m.most ? b : m.most;
+                    }
+                m = reduce(m);
+                q.ok = m.most < 0x7f800000u;
+                const int e = q.ok && m.most ? -ilogbf(__uint_as_float(m.most)) : 0;
+                const float p0 = pow2(e / 2), p1 = pow2(e - e / 2);
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+                for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) h[c][j] = h[c][j] * p0 * p1;
-            s = stat();
-            ok = ok && s.most < 0x7f800000u;
-            const double q0 = p0, q1 = p1;
-            double d = (double)__uint_as_float(s.most) / 127.0;
-            if constexpr (NORM) d /= sqrt((double)s.ss / k + (double)a.eps * q0 * q0 * q1 * q1);
-            else d = d / q0 / q1;
-            scale = ok ? (float)d : __uint_as_float(0x7fc00000u);
+                    for (int j = 0; j < 8; ++j) h[c][j] = h[c][j] * p0 * p1;
+                s = stat();
+                q.ok = q.ok && s.most < 0x7f800000u;
+                const float top = __uint_as_float(s.most);
+                const double d0 = p0, d1 = p1;
+                q.scale = q.ok ? (float)((double)top / 127.0 / sqrt((double)s.ss / k + (double)a.eps * d0 * d0 * d1 * d1)) : __uint_as_float(0x7fc00000u);
+                q.inv = q.ok && top > 0.f ? 127.f / top : 0.f;
+                q.p0 = q.p1 = 1.f;
+            }
         }
-        const float top = __uint_as_float(s.most), inv = ok && top > 0.f ? 127.f / top : 0.f;
         int8_t* codes = a.codes + (size_t)row * a.pitch;
         gain([&](int c, const float* gc) {
             if (at[c] >= a.pitch) return;
-            uint32_t q[8];
+            uint32_t v[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)   // (a product with NaN or infinity is not converted)
-                q[j] = ok ? (uint32_t)(int)rintf((NORM ? h[c][j] * gc[j] : h[c][j]) * inv) & 255u : 0u;
-            const u32x2_t o = {q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24, q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24};
+            for (int j = 0; j < 8; ++j) v[j] = row_code(q, NORM ? h[c][j] * gc[j] : h[c][j]);
+            const u32x2_t o = {v[0] | v[1] << 8 | v[2] << 16 | v[3] << 24, v[4] | v[5] << 8 | v[6] << 16 | v[7] << 24};
             *reinterpret_cast<u32x2_t*>(codes + at[c]) = o;
         });
-        if (lane == 0 && (WPR == 1 || wv == 0)) a.scales[row] = scale;
+        if (lane == 0 && (WPR == 1 || wv == 0)) a.scales[row] = q.scale;
     }
 }
 
@@ -222,7 +221,7 @@ template <typename T, bool NORM, int WPR, int C>
 hipError_t launch_cfg(const RowArgs& a, hipStream_t s) {
     constexpr int RPB = WPR == 1 ? 4 : 1, THREADS = WPR == 1 ? 256 : WPR * 64;
     // Blocks that the chip holds at once walk over the rows; without a gain to keep, a wide row is a block of its own, so that a last
-    // round is not waited for (us, walking / a block per row: norm of 8 192 x 8 192 91 / 105, codes of 9 600 x 12 544 103 / 93).
+    // round is not waited for (us, walking / a block per row: norm of 8 192 x 8 192 91 / 105, codes of 9 600 x 12 544 89 / 74).
     const long long groups = ((long long)a.rows + RPB - 1) / RPB, most = !NORM && WPR > 1 ? 1 << 22 : 256ll * 2048 / THREADS;
     hipLaunchKernelGGL((rows_i8_kernel<T, NORM, WPR, C>), dim3((unsigned)(groups < most ? groups : most)), dim3(THREADS), 0, s, a);
     return hipGetLastError();
@@ -230,8 +229,8 @@ hipError_t launch_cfg(const RowArgs& a, hipStream_t s) {
 
 // Up to 1024 values a wavefront per row, which needs no barrier (9 600 x 1 024 norm in us: one wavefront 13.1, two 13.5, four
 // 16.3).  Beyond, a row is spread until a lane has eight values of it for the norm, which holds most registers (us, 8 / 16 / 32 values per
-// lane: 16 384 x 4 096 91 / 98 / 126, 8 192 x 8 192 91 / 96 / 111), and sixteen or 32 without it (8 192 x 8 192 38 / 35 / 35, 16 384 x 4 096 36 / 32 /
-// 34); with few rows the wider spread is the quicker too (one row of 8 192: norm 4.4 / 4.4 / 6.1, codes 3.4 / 3.4 / 3.9).
+// lane: 16 384 x 4 096 90 / 98 / 126, 8 192 x 8 192 91 / 96 / 111), and sixteen or 32 without it (8 192 x 8 192 38 / 33 / 35, 16 384 x 4 096 36 / 32 /
+// 34); with few rows the wider spread is the quicker too (one row of 8 192: norm 4.3 / 4.4 / 6.1, codes 3.4 / 3.4 / 3.9).
 template <typename T, bool NORM>
 hipError_t launch_rows(const RowArgs& a, hipStream_t s) {
     const int k = a.k;

@@ -202,6 +202,10 @@ hipError_t launch_nms(const float* boxes, const int32_t* counts, int n, int cap,
 // ---------------------------------------------------------------- ROI head
 hipError_t launch_roialign(const void* feat, const float* rois, int n, int post, int Hk, int Wk, int Ch, int stride, int P,
                            int precision, void* out, hipStream_t s);
+// The same features as rows of 8-bit codes [n*post][thia_i8_pitch(P*P*Ch)] with scales [n*post], in calls where that pays.
+bool roialign_codes_pay(int n, int post, int Ch, int P, int precision);
+hipError_t launch_roialign_codes(const void* feat, const float* rois, int n, int post, int Hk, int Wk, int Ch, int stride, int P, int precision,
+                                 int8_t* codes, float* scales, hipStream_t s);
 // cls [n*post,Kc] logits, deltas [n*post,4Kc], rois [n,post,4] -> scores [n,post,Kc], boxes [n,post,Kc,4]
 hipError_t launch_scores_boxes(const float* cls, const float* deltas, const float* rois, int n, int post, int Kc, float imgW,
                                float imgH, float* scores, float* boxes, hipStream_t s);
