@@ -607,7 +607,7 @@ def _i8_start(x, out):
         raise ThiaError(-3, "rows of codes hold 1 to 65536 values")
     pitch = -(-k // 128) * 128
     if out is None:
-        return precision, ldx, rows, k, device, torch.empty((rows, pitch), dtype=torch.int8, device=device), torch.empty(rows, dtype=torch.float32, device=device)
+        return precision, ldx, rows, k, device, x.new_empty((rows, pitch), dtype=torch.int8), x.new_empty(rows, dtype=torch.float32)
     _i8_codes(*out, rows, pitch, device)
     return (precision, ldx, rows, k, device, *out)
 
@@ -630,7 +630,7 @@ def rms_norm_i8(x, gain, eps=1e-6, residual=None, sum_out=None, out=None):
     if residual is not None:
         ldr, rp = _i8_rows("residual", residual, x.dtype, device, x.shape), residual.data_ptr()
         if sum_out is None:
-            sum_out = torch.empty((rows, k), dtype=x.dtype, device=device)
+            sum_out = x.new_empty((rows, k))
         else:
             lds = _i8_rows("sum_out", sum_out, x.dtype, device, x.shape)
         sp = sum_out.data_ptr()
@@ -686,7 +686,7 @@ class LinearI8:
         if residual is not None:
             ldr, rp = _i8_rows("residual", residual, dtype, device, (rows, self.n)), residual.data_ptr()
         if out is None:
-            out = torch.empty((rows, self.n), dtype=dtype, device=device)
+            out = scales.new_empty((rows, self.n), dtype=dtype)
         else:
             ldo = _i8_rows("out", out, dtype, device, (rows, self.n))
         _i8_call(device, lib().thia_linear_i8_run, self._h, codes.data_ptr(), scales.data_ptr(), rows, rp, ldr, 1 if relu else 0, 0 if out_f32 else 1,

@@ -379,13 +379,17 @@ int thia_linear_i8_run(const thia_linear_i8* l, const int8_t* codes, const float
     a.vec = l->n % 8 == 0 && wide(out, ldo) && (!residual || wide(residual, ldr));
     // rows in as many launches as keep the number of threads of each below 2^32 (a multiple of every tile's rows)
     const int most = (int)((1ll << 33) / l->n / 768 < 2048 ? (1ll << 33) / l->n / 768 : 2048) * 768;
-    for (long long m = 0; m < rows && e == hipSuccess; m += most) {
-        a.rows = rows - m < most ? (int)(rows - m) : most;
-        a.x = codes + m * l->pitch;
-        a.xscale = scales + m;
-        a.res = residual ? static_cast<const char*>(residual) + m * ldr * (long long)elem : nullptr;
-        a.out = static_cast<char*>(out) + m * ldo * (long long)elem;
-        e = precision ? launch_linear<bf16_t>(a, (hipStream_t)hip_stream) : launch_linear<float>(a, (hipStream_t)hip_stream);
+    try {
+        for (long long m = 0; m < rows && e == hipSuccess; m += most) {
+            a.rows = rows - m < most ? (int)(rows - m) : most;
+            a.x = codes + m * l->pitch;
+            a.xscale = scales + m;
+            a.res = residual ? static_cast<const char*>(residual) + m * ldr * (long long)elem : nullptr;
+            a.out = static_cast<char*>(out) + m * ldo * (long long)elem;
+            e = precision ? launch_linear<bf16_t>(a, (hipStream_t)hip_stream) : launch_linear<float>(a, (hipStream_t)hip_stream);
+        }
+    } catch (...) {   // (the table of raised LDS limits)
+        return i8_fail(THIA_E_NOMEM, "out of host memory");
     }
     return e == hipSuccess ? THIA_OK : i8_fail(THIA_E_HIP, hipGetErrorString(e));
 }

@@ -222,7 +222,7 @@ hipError_t launch_cfg(const RowArgs& a, hipStream_t s) {
     constexpr int RPB = WPR == 1 ? 4 : 1, THREADS = WPR == 1 ? 256 : WPR * 64;
     // Blocks that the chip holds at once walk over the rows; without a gain to keep, a wide row is a block of its own, so that a last
     // round is not waited for (us, walking / a block per row: norm of 8 192 x 8 192 91 / 105, codes of 9 600 x 12 544 89 / 74).
-    const long long groups = ((long long)a.rows + RPB - 1) / RPB, most = !NORM && WPR > 1 ? 1 << 22 : 256ll * 2048 / THREADS;
+    const long long groups = ((long long)a.rows + RPB - 1) / RPB, most = !NORM && WPR > 1 ? 1 << 21 : 256ll * 2048 / THREADS;
     hipLaunchKernelGGL((rows_i8_kernel<T, NORM, WPR, C>), dim3((unsigned)(groups < most ? groups : most)), dim3(THREADS), 0, s, a);
     return hipGetLastError();
 }

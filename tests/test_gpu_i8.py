@@ -410,6 +410,29 @@ def test_block_captured_and_on_other_streams():
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_two_threads_at_once():
+    """Calls from two threads, each on a stream of its own, with one layer: nothing is shared between calls."""
+    import threading
+    (up, down), _, gain = block_parts(300, 512, 1024)
+    r = rows_of(4, 300, 512, BF)
+    xs = [rows_of(30 + i, 300, 512, BF) for i in range(2)]
+    want = [block(x, r, gain, up, down)[-1] for x in xs]
+    torch.cuda.synchronize()
+    got = [[], []]
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                got[i].append(block(xs[i], r, gain, up, down)[-1])
+            torch.cuda.current_stream().synchronize()
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert all(len(g) == 20 and all(torch.equal(v, w) for v in g) for g, w in zip(got, want))
+
+
 # ---------------------------------------------------------------- the box head in 8 bits
 def head_layers(spec, blob, ep):
     """Exit ep's wide layers from the blob, in the element type and order the library keeps them, and the predictors in 64 bits."""
