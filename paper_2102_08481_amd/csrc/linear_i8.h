@@ -108,16 +108,32 @@ __device__ inline void finish_four(const LinearArgs& a, const i32x4_t& s, size_t
 // l % 32.  32 rows at a time are parked in the wavefront's own FINISH_LDS bytes of LDS and read back by rows, so that accesses
 // of memory cover whole lines.  m0 + r0: the wavefront's first row; `rows` of the block's rows exist; nw: the first channel.
 constexpr int FINISH_PITCH = 64 * 4 + 16, FINISH_LDS = 32 * FINISH_PITCH;
+// Scales and biases of the block's channels (256 at most) and scales of its ROWS rows lie in LDS: one request in front of all others by
+// each of a few wavefronts (the rows' by single values: their address may be any multiple of 4).  Fetched by the epilogue they
+// were a trip to memory for the channels and one for every 32 rows, 4 of the 10 us that a 256 x 256 block took beside its K tiles.
+constexpr int FACTORS_LDS = 3 * 1024;
+template <int ROWS>
+__device__ inline void request_factors(const LinearArgs& a, int wv, int lane, unsigned char* to, int n0, size_t m0, int rows) {
+    typedef __attribute__((address_space(3))) unsigned char lds_byte;
+    if (wv < 2) {
+        const uint32_t chans = (uint32_t)((a.n + 255) / 256 * 256 - n0) * 4;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer((wv ? a.bias : a.wscale) + n0, chans), (lds_byte*)(to + wv * 1024), 16, lane * 16, 0, 0, 0);
+    } else if (wv < 2 + ROWS / 64) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(a.xscale + m0, (uint32_t)rows * 4), (lds_byte*)(to + 2048 + (wv - 2) * 256), 4, (wv - 2) * 256 + lane * 4, 0, 0, 0);
+    }
+}
 template <typename T, int TM>
-__device__ inline void finish_rows(const LinearArgs& a, const i32x16_t (&acc)[2][TM], unsigned char* ep, int lane, size_t m0, int r0, int rows, int nw) {
-    const int frag_row = lane & 31;
+__device__ inline void finish_rows(const LinearArgs& a, const i32x16_t (&acc)[2][TM], unsigned char* ep, const unsigned char* factors, int lane, size_t m0, int r0, int rows,
+                                   int c0, int n0) {
+    const int frag_row = lane & 31, nw = n0 + c0;
     f32x4_t ws[2][4], bs[2][4];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {   // (scales and biases have room for whole blocks)
-            ws[i][v] = *reinterpret_cast<const f32x4_t*>(a.wscale + nw + i * 32 + 8 * v + 4 * (lane >> 5));
-            bs[i][v] = *reinterpret_cast<const f32x4_t*>(a.bias + nw + i * 32 + 8 * v + 4 * (lane >> 5));
+        for (int v = 0; v < 4; ++v) {
+            const unsigned char* at = factors + (c0 + i * 32 + 8 * v + 4 * (lane >> 5)) * 4;
+            ws[i][v] = *reinterpret_cast<const f32x4_t*>(at);
+            bs[i][v] = *reinterpret_cast<const f32x4_t*>(at + 1024);
         }
     // bf16: the residual of 32 rows is fetched while the 32 in front of them are finished (us, fetched in turn / ahead: 16384 x 1024 x 4096
     // 129 / 107, 4096 x 4096 x 1024 25.8 / 23.8; fp32, whose residual takes twice the registers, 154 / 164: in turn)
@@ -143,7 +159,7 @@ __device__ inline void finish_rows(const LinearArgs& a, const i32x16_t (&acc)[2]
             for (int it = 0; it < 4; ++it) now[it] = next[it];
             if constexpr (j + 1 < TM) fetch(j + 1);
         }
-        const float xs = rj + frag_row < rows ? a.xscale[m0 + rj + frag_row] : 0.f;
+        const float xs = *reinterpret_cast<const float*>(factors + 2048 + (rj + frag_row) * 4);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll

@@ -81,6 +81,8 @@ __global__ __launch_bounds__(512, 1) void linear_large_kernel(const LinearArgs a
     };
     constexpr std::integral_constant<int, 0> H0{};
     constexpr std::integral_constant<int, 1> H1{};
+    unsigned char* factors = smem + 128 * 1024;
+    request_factors<BM>(a, wv, lane, factors, n0, m0, rows);
     request_w(0, 0, 0);
     request_w(1, 0, 0);
     request_x(H0, 0, 0);
@@ -190,13 +192,13 @@ __global__ __launch_bounds__(512, 1) void linear_large_kernel(const LinearArgs a
     if (wv < 4) barrier();
     // (every wavefront has read its last fragments and no request is on its way: LDS is free)
 
-    finish_rows<T, TM>(a, acc, smem + (size_t)wv * FINISH_LDS, lane, m0, wm * WM, rows, n0 + wn * 64);
+    finish_rows<T, TM>(a, acc, smem + (size_t)wv * FINISH_LDS, factors, lane, m0, wm * WM, rows, wn * 64, n0);
 #endif
 }
 
 template <typename T, int BM>
 hipError_t launch_large(const LinearArgs& a, hipStream_t s) {
-    const size_t lds = 128 * 1024;
+    const size_t lds = 128 * 1024 + FACTORS_LDS;
     auto kern = linear_large_kernel<T, BM>;
     const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds);
     if (e != hipSuccess) return e;

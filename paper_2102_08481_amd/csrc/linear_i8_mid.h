@@ -16,7 +16,7 @@ __global__ __launch_bounds__(BM * BN / 64) void linear_mid_kernel(const LinearAr
     constexpr int NW = BM * BN / 4096, WAVES_M = BM / 64;
     constexpr int FW = BN / 8 / NW, FX = BM / 8 / NW, PER = FW + FX;   // requests of a thread per K tile
     constexpr uint32_t BUF = (BM + BN) * 128, XOFF = BN * 128;         // a place of the ring: weights, rows
-    static_assert(FW * NW * 8 == BN && FX * NW * 8 == BM && NW % 2 == 0 && R >= 3 && (R - 2) * PER < 64, "requests are shared evenly, vmcnt counts to 63");
+    static_assert(FW * NW * 8 == BN && FX * NW * 8 == BM && NW % 2 == 0 && NW >= 2 + BM / 64 && R >= 3 && (R - 2) * PER < 64, "requests are shared evenly, vmcnt counts to 63");
     extern __shared__ __align__(128) unsigned char smem[];
 
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -96,6 +96,8 @@ __global__ __launch_bounds__(BM * BN / 64) void linear_mid_kernel(const LinearAr
             __builtin_amdgcn_sched_barrier(0);
         });
     };
+    unsigned char* factors = smem + R * BUF;
+    request_factors<BM>(a, wv, lane, factors, n0, m0, rows);
     for (int r = 0; r < R; ++r) static_for<0, PER>([&](auto uc) { request_one(uc, r, r * BUF); });
     {
         constexpr int n = (R - 1) * PER;
@@ -117,13 +119,13 @@ __global__ __launch_bounds__(BM * BN / 64) void linear_mid_kernel(const LinearAr
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    finish_rows<T, 2>(a, acc, smem + (size_t)wv * FINISH_LDS, lane, m0, wm * 64, rows, n0 + wn * 64);
+    finish_rows<T, 2>(a, acc, smem + (size_t)wv * FINISH_LDS, factors, lane, m0, wm * 64, rows, wn * 64, n0);
 #endif
 }
 
 template <typename T, int BM, int BN, int R>
 hipError_t launch_mid(const LinearArgs& a, hipStream_t s) {
-    const size_t lds = (size_t)R * (BM + BN) * 128;
+    const size_t lds = (size_t)R * (BM + BN) * 128 + FACTORS_LDS;
     auto kern = linear_mid_kernel<T, BM, BN, R>;
     const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds);
     if (e != hipSuccess) return e;

@@ -206,6 +206,8 @@ def test_linear_ragged(rows, k, n, dtype):
     codes, scales = codes_of(k, rows, k)
     out = thia.thia_linear_i8_run(layer, codes, scales, True, out_f32=dtype is F)
     check_product(out, codes, scales, w, ws, b, k, True)
+    moved = torch.cat([scales[:1], scales])[1:]   # 4 bytes off
+    assert torch.equal(thia.thia_linear_i8_run(layer, codes, moved, True, out_f32=dtype is F), out)
     res = rows_of(9, rows, n + 3, dtype)[:, 1:n + 1]
     want = thia.thia_linear_i8_run(layer, codes, scales, False, res.contiguous(), dtype is F)
     check_product(want, codes, scales, w, ws, b, k, False, res)
