@@ -71,15 +71,18 @@ __device__ inline void relu_if(int relu, float (&v)[N]) {
     }
 }
 
-// ---- epilogue of the smaller tiles: four channels from ch (a multiple of 4) on of row m, if it exists.
+// ---- epilogue of the smaller tiles: four channels from ch (a multiple of 4) on of row m, if it exists.  Their scales and biases are
+// fetched in front of the contraction.
+struct ChannelFactors { f32x4_t ws, b; };
+__device__ inline ChannelFactors channel_factors(const LinearArgs& a, int ch) {   // (there is room for whole blocks)
+    return {*reinterpret_cast<const f32x4_t*>(a.wscale + ch), *reinterpret_cast<const f32x4_t*>(a.bias + ch)};
+}
 template <typename T>
-__device__ inline void finish_four(const LinearArgs& a, const i32x4_t& s, size_t m, bool exists, int ch) {
+__device__ inline void finish_four(const LinearArgs& a, const i32x4_t& s, float xs, const ChannelFactors& f, size_t m, bool exists, int ch) {
     if (!exists || ch >= a.n) return;
-    const float xs = a.xscale[m];
-    const f32x4_t ws = *reinterpret_cast<const f32x4_t*>(a.wscale + ch), b = *reinterpret_cast<const f32x4_t*>(a.bias + ch);
     float v[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = scaled(s[e], xs, ws[e], b[e]);
+    for (int e = 0; e < 4; ++e) v[e] = scaled(s[e], xs, f.ws[e], f.b[e]);
     T* out = static_cast<T*>(a.out) + m * a.ldo + ch;
     const T* res = a.res ? static_cast<const T*>(a.res) + m * a.ldr + ch : nullptr;
     if (a.vec) {

@@ -44,6 +44,14 @@ __global__ __launch_bounds__(64 * W) void linear_small_kernel(const LinearArgs a
     for (int i = 0; i < TN; ++i) w_off[i] = (uint32_t)(i * 32 * a.pitch + lane * 16);
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) x_at[kk] = lds0 + (uint32_t)((lane & 31) * 128) + (uint32_t)(((2 * kk + (lane >> 5)) ^ (lane & 7) ^ ((lane >> 3) & 1)) * 16);
+    // results of a thread: the same four channels of EACH rows
+    constexpr int EACH = SUBS * 256 / (64 * W), STEP = 64 * W / (8 * TN);
+    static_assert(SUBS * 256 % (64 * W) == 0 && 64 * W % (8 * TN) == 0, "results are shared evenly");
+    const int my_g = threadIdx.x % (8 * TN), my_row = threadIdx.x / (8 * TN), my_ch = n0 + my_g * 4;
+    const ChannelFactors factors = channel_factors(a, my_ch);
+    float xs[EACH];
+#pragma unroll
+    for (int r = 0; r < EACH; ++r) xs[r] = my_row + r * STEP < rows ? a.xscale[(size_t)m0 + my_row + r * STEP] : 0.f;
     i32x16_t acc[TN][TM] = {};
     u32x4_t w[SLOTS][TN][4];
     // Piece kt into place s.  Descriptors end behind the tile's last row and channel, and behind the last piece are empty: what
@@ -107,13 +115,14 @@ __global__ __launch_bounds__(64 * W) void linear_small_kernel(const LinearArgs a
             for (int v = 0; v < 4; ++v)
                 *reinterpret_cast<i32x4_t*>(mine + (i * TM + j) * SUB + 2 * v * GROUP) = i32x4_t{acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]};
     __syncthreads();
-    for (int t = threadIdx.x; t < SUBS * 256; t += 64 * W) {   // four channels of a row each
-        const int g = t % (8 * TN), row = t / (8 * TN), sub = (g >> 3) * TM + (row >> 5);
-        const unsigned char* at = smem + (size_t)sub * SUB + (g & 7) * GROUP + (row & 31) * 16;
+#pragma unroll
+    for (int r = 0; r < EACH; ++r) {
+        const int row = my_row + r * STEP, sub = (my_g >> 3) * TM + (row >> 5);
+        const unsigned char* at = smem + (size_t)sub * SUB + (my_g & 7) * GROUP + (row & 31) * 16;
         i32x4_t s = *reinterpret_cast<const i32x4_t*>(at);
 #pragma unroll
         for (int w = 1; w < W; ++w) s += *reinterpret_cast<const i32x4_t*>(at + (size_t)w * REGION);
-        finish_four<T>(a, s, (size_t)m0 + row, row < rows, n0 + g * 4);
+        finish_four<T>(a, s, xs[r], factors, (size_t)m0 + row, row < rows, my_ch);
     }
 #endif
 }

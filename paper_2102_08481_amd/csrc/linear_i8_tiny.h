@@ -32,6 +32,9 @@ __global__ __launch_bounds__(64 * W) void linear_tiny_kernel(const LinearArgs a)
             q.x[j] = __builtin_amdgcn_raw_buffer_load_b128(rx, x_off, kt * 128 + j * 64, 0);
         }
     };
+    const int row = lane & 15, ch = (int)tile_n * 16 + (lane >> 4) * 4;   // of the lane's four results (the first wavefront's)
+    const ChannelFactors factors = channel_factors(a, ch);
+    const float xs = row < rows ? a.xscale[(size_t)m0 + row] : 0.f;
     i32x4_t acc = {};
     static_for<0, D>([&](auto s) { fetch(p[decltype(s)::value], wv + decltype(s)::value * W); });
     for (int kt = wv; kt < KT;) {
@@ -54,7 +57,7 @@ __global__ __launch_bounds__(64 * W) void linear_tiny_kernel(const LinearArgs a)
     i32x4_t s = part[0][lane];
 #pragma unroll
     for (int w = 1; w < W; ++w) s += part[w][lane];
-    finish_four<T>(a, s, (size_t)m0 + (lane & 15), (lane & 15) < rows, (int)tile_n * 16 + (lane >> 4) * 4);
+    finish_four<T>(a, s, xs, factors, (size_t)m0 + row, row < rows, ch);
 #endif
 }
 
