@@ -17,8 +17,8 @@
 //
 // 8192 x 8192 x 8192 takes 423 us (2.6 POP/s; a library's product of 8-bit integers without scales 524), 9600 x 12544 x 1024 on 200 blocks of
 // 192 x 256 107 us (2.3 POP/s; 197).  The matrix pipes are busy in 74 % of the cycles there, and the chip's clock comes down to 1.4 GHz under them:
-// a K tile of 256 x 256 takes 0.96 us while a few CUs work and 1.6 when all do.  About 10 us per block do not grow with K (first
-// operands, results: 4096 x 1024 x 4096 takes 23 us for 14 us of products).
+// a K tile of 256 x 256 takes 0.96 us while a few CUs work and 1.6 when all do.  About 8 us per block do not grow with K (launch,
+// first operands, results, which all blocks of a round write at once: 4096 x 1024 x 4096 takes 22 us for 14 us of products).
 //
 // Part of linear_i8.h, which includes it once.
 template <typename T, int BM>
