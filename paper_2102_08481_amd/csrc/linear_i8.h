@@ -40,18 +40,18 @@ struct LinearArgs {
     int vec;   // rows of out and res take accesses of 16 bytes: n a multiple of 8, addresses and pitches of 16 bytes
 };
 
-// int8 rows [n][ld] -> fragments; one thread per 16 bytes
+// int8 rows [n][ld] -> fragments; 16 bytes at a time
 __global__ void pack_i8_kernel(const int8_t* __restrict__ src, long long ld, int n, int k, int pitch, int8_t* __restrict__ dst, size_t pieces) {
-    const size_t p = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (p >= pieces) return;
-    const int lane = (int)(p & 63);
-    const size_t f = p >> 6;
-    const int ks = (int)(f % (pitch / 32));
-    const long long row = (long long)(f / (pitch / 32)) * 32 + (lane & 31);
-    const int k0 = ks * 32 + (lane >> 5) * 16;
-    union { int8_t b[16]; i32x4_t v; } o;
-    for (int j = 0; j < 16; ++j) o.b[j] = row < n && k0 + j < k ? src[row * ld + k0 + j] : (int8_t)0;
-    *reinterpret_cast<i32x4_t*>(dst + p * 16) = o.v;
+    for (size_t p = (size_t)blockIdx.x * blockDim.x + threadIdx.x; p < pieces; p += (size_t)gridDim.x * blockDim.x) {
+        const int lane = (int)(p & 63);
+        const size_t f = p >> 6;
+        const int ks = (int)(f % (pitch / 32));
+        const long long row = (long long)(f / (pitch / 32)) * 32 + (lane & 31);
+        const int k0 = ks * 32 + (lane >> 5) * 16;
+        union { int8_t b[16]; i32x4_t v; } o;
+        for (int j = 0; j < 16; ++j) o.b[j] = row < n && k0 + j < k ? src[row * ld + k0 + j] : (int8_t)0;
+        *reinterpret_cast<i32x4_t*>(dst + p * 16) = o.v;
+    }
 }
 
 __device__ inline __amdgpu_buffer_rsrc_t buffer(const void* p, uint32_t bytes) {
@@ -284,7 +284,8 @@ int fill_layer(thia_linear_i8* l, const int8_t* codes, long long ld, const float
     if (e == hipSuccess && bias) e = hipMemcpy(l->scale_bias + floats, bias, (size_t)l->n * 4, hipMemcpyDefault);
     if (e == hipSuccess) {
         const size_t pieces = bytes / 16;
-        hipLaunchKernelGGL(pack_i8_kernel, dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, nullptr, codes, ld, l->n, l->k, l->pitch, l->w, pieces);
+        const size_t blocks = (pieces + 255) / 256;
+        hipLaunchKernelGGL(pack_i8_kernel, dim3((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20)), dim3(256), 0, nullptr, codes, ld, l->n, l->k, l->pitch, l->w, pieces);
         e = hipGetLastError();
     }
     if (e == hipSuccess) e = hipStreamSynchronize(nullptr);

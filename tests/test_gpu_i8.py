@@ -250,6 +250,18 @@ def test_offsets_beyond_32_bits(rows, k):
     assert all(torch.equal(a[-40:], b) for a, b in zip((codes, scales, total), want))
 
 
+def test_weights_beyond_32_bits():
+    """A layer of more than 2^32 bytes: its last channels are those of a layer of them alone."""
+    import paper_2102_08481_amd as thia
+    n, k = 70003, 65536
+    w = torch.ones((n, k), dtype=torch.int8, device="cuda")
+    w[-50:] = torch.randint(-127, 128, (50, k), device="cuda", dtype=torch.int8)
+    one = torch.ones(n, device="cuda")
+    codes, scales = codes_of(2, 37, k)
+    out = thia.thia_linear_i8_run(thia.thia_linear_i8_load_codes(w, one), codes, scales)
+    assert torch.equal(out[:, -50:], thia.thia_linear_i8_run(thia.thia_linear_i8_load_codes(w[-50:].contiguous(), one[:50]), codes, scales))
+
+
 @pytest.mark.parametrize("n,out_f32", [(30007, True), (60000, False)])
 def test_results_beyond_32_bits(n, out_f32):
     import paper_2102_08481_amd as thia
