@@ -465,8 +465,9 @@ int thia_classifier_op_unit(thia_classifier* c, const void* feat, int n, int HW,
  * Rows of 8-bit whole numbers with one scale each, what makes them, and the product of two such matrices: the wide layers of a
  * box head (or any other matrix product over rows) on the 8-bit matrix instructions, with half the bytes of bf16.
  *
- * A row y of k values is held as codes q[j] in -127..127 and a scale s, standing for q[j] * s: s = max|y| / 127 and q[j] =
- * y[j] / s rounded to nearest (ties to even).  A row of zeros has scale 0 and codes 0; a row with a NaN or an infinity has
+ * A row y of k values is held as codes q[j] in -127..127 and a scale s, standing for q[j] * s: s = max|y| / 127 in fp32 and q[j] =
+ * 127 y[j] / max|y|, the quotient in fp32, rounded to nearest (ties to even; of bf16 rows every code is the nearest, of fp32 rows a
+ * quotient within 2^-18 of a tie may count as one).  A row of zeros has scale 0 and codes 0; a row with a NaN or an infinity has
  * scale NaN and codes 0, so that whatever is computed from it is NaN.  Codes lie in rows of thia_i8_pitch(k) bytes (k
  * rounded up to whole lines of 128), codes dev int8 [rows, pitch] and 16-byte aligned; the bytes behind column k are written as
  * zeros and never matter when read.  k is 1..65536.

@@ -121,20 +121,39 @@ __device__ inline bool iou_over(const Box& a, const Box& b, float thr) {
 // ---- rows in 8 bits: scale and codes of a row from the bits of its largest size (infinity and NaN sort last)
 __device__ inline uint32_t size_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 __device__ inline float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
-// codes are v p0 p1 inv, rounded to nearest even; p0 p1 brings the largest value of a row that leaves the plain range to 1..2
-struct RowScale { float scale, inv, p0, p1; bool ok; };
+// Codes are the quotient 127 v / top in fp32, rounded to nearest even.  127 / top is held as two numbers, inv + rest: with one alone half of the
+// largest value (and whatever else lies on the border of two codes) fell to either side of it.  With two the quotient is the true one rounded
+// once, so a border stays one, and of bf16 rows every code is the nearest: a quotient between 2^(n-1) and 2^n that is no border lies more than
+// 2^(n-17) from one (mantissas of 8 bits), and rounding moves it by at most 2^(n-25).
+struct RowScale { float inv, rest; bool ok; };   // ok: the row is finite
+// top is 0, or 1e-30 to 1e30; `most` is the same in all lanes of a wavefront.
 __device__ inline RowScale row_scale(uint32_t most) {
-    const float top = __uint_as_float(most);
-    if (top >= 1e-30f && top <= 1e30f) return {top / 127.f, 127.f / top, 1.f, 1.f, true};
-    RowScale r = {__uint_as_float(0x7fc00000u), 0.f, 1.f, 1.f, most < 0x7f800000u};
-    if (!r.ok) return r;
-    const int e = most ? -ilogbf(top) : 0;
-    r.p0 = pow2(e / 2);
-    r.p1 = pow2(e - e / 2);
-    r.scale = (float)((double)top / 127.0);
-    r.inv = most ? 127.f / (top * r.p0 * r.p1) : 0.f;
+    most = __builtin_amdgcn_readfirstlane(most);
+    RowScale r = {0.f, 0.f, most < 0x7f800000u};
+    if (most && r.ok) {
+        const float top = __uint_as_float(most);
+        r.inv = 127.f / top;
+        r.rest = __builtin_fmaf(-r.inv, top, 127.f) * (r.inv / 127.f);   // (the first factor exact)
+    }
     return r;
 }
-__device__ inline uint32_t row_code(const RowScale& r, float v) { return r.ok ? (uint32_t)(int)rintf(v * r.p0 * r.p1 * r.inv) & 255u : 0u; }
+// Codes of four values in the bytes of a word.  Behind the addition a number's lowest bits are the nearest whole number to it.
+__device__ inline uint32_t row_codes4(const RowScale& r, const float* v) {
+    if (!r.ok) return 0u;
+    uint32_t c[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[j] = __float_as_uint(__builtin_fmaf(v[j], r.inv, v[j] * r.rest) + 12582912.f);
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[3], c[2], 0x0c0c0400u), __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400u), 0x05040100u);
+}
+// Of rows as they are: the scale (NaN if the row is not finite) and the power of two that brings rows outside 1e-30 to 1e30 back into it, 1 for all others.
+__device__ inline float row_step(uint32_t most, float& power) {
+    most = __builtin_amdgcn_readfirstlane(most);
+    const float top = __uint_as_float(most);
+    power = 1.f;
+    if (top >= 1e-30f && top <= 1e30f) return top / 127.f;
+    if (most >= 0x7f800000u) return __uint_as_float(0x7fc00000u);
+    power = top < 1.f ? pow2(100) : pow2(-100);
+    return (float)((double)top / 127.0);
+}
 
 }  // namespace thia

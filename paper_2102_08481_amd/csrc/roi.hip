@@ -153,28 +153,30 @@ __global__ __launch_bounds__(256) void roialign_kernel(const T* __restrict__ fea
         if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = most;
         __syncthreads();
         for (int w = 0; w < 4; ++w) most = s_most[w] > most ? s_most[w] : most;
-        const RowScale q = row_scale(most);
+        float p;
+        const float step = row_step(most, p);
+        const RowScale q = row_scale(size_bits(__uint_as_float(most) * p));
         int8_t* row = codes + (size_t)roi * pitch;
         for (int i = threadIdx.x; i < nb * runs; i += 256) {
             const uint4 v = held[i];
             const uint32_t wd[4] = {v.x, v.y, v.z, v.w};
-            uint32_t c[VEC];
+            float y[VEC];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if constexpr (sizeof(T) == 2) {
-                    c[2 * e] = row_code(q, __uint_as_float(wd[e] << 16));
-                    c[2 * e + 1] = row_code(q, __uint_as_float(wd[e] & 0xffff0000u));
+                    y[2 * e] = __uint_as_float(wd[e] << 16) * p;
+                    y[2 * e + 1] = __uint_as_float(wd[e] & 0xffff0000u) * p;
                 } else {
-                    c[e] = row_code(q, __uint_as_float(wd[e]));
+                    y[e] = __uint_as_float(wd[e]) * p;
                 }
             }
             if constexpr (sizeof(T) == 2)
-                *reinterpret_cast<uint2*>(row + 8 * i) = make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
+                *reinterpret_cast<uint2*>(row + 8 * i) = make_uint2(row_codes4(q, y), row_codes4(q, y + 4));
             else
-                *reinterpret_cast<uint32_t*>(row + 4 * i) = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
+                *reinterpret_cast<uint32_t*>(row + 4 * i) = row_codes4(q, y);
         }
         for (int i = nb * Ch + threadIdx.x; i < pitch; i += 256) row[i] = 0;
-        if (threadIdx.x == 0) scales[roi] = q.scale;
+        if (threadIdx.x == 0) scales[roi] = step;
     }
 }
 

@@ -73,9 +73,10 @@ struct RowArgs {
 // reads from the caches (us, held / read: 9 600 x 1 024 12.8 / 13.9, 16 384 x 4 096 in two pieces 99 / 119, 4 096 x 16 384 in four 138 / 109).
 constexpr int kHold = 2;
 // A row per WPR wavefronts, 8 C values of it per lane, in registers from the one load to the codes' store; with WPR 1 four rows
-// per block.  Blocks walk over the rows, so that the gain stays in registers.
+// per block.  Blocks walk over the rows, so that the gain stays in registers.  (Eight wavefronts per SIMD with few values per lane: 64 registers, so
+// that two blocks of sixteen wavefronts fit a CU.)
 template <typename T, bool NORM, int WPR, int C>
-__global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void rows_i8_kernel(const RowArgs a) {
+__global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64, NORM && C == 1 ? 8 : 1) void rows_i8_kernel(const RowArgs a) {
     constexpr int RPB = WPR == 1 ? 4 : 1;
     __shared__ RowStat red[2][WPR];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -160,13 +161,21 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void rows_i8_kernel(cons
             return reduce(s);
         };
         RowStat s = stat();
-        RowScale q;
+        float scale;
         if constexpr (!NORM) {
-            q = row_scale(s.most);
+            float p;
+            scale = row_step(s.most, p);
+            if (p != 1.f) {
+                s.most = size_bits(__uint_as_float(s.most) * p);
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) h[c][j] *= p;
+            }
         } else {
             const float most = __uint_as_float(s.most);
             if (most >= 1e-30f && most <= 1e30f && s.ss >= 1e-20f && s.ss <= 1e30f) {
-                q = {most / 127.f / sqrtf(s.ss / (float)k + a.eps), 127.f / most, 1.f, 1.f, true};
+                scale = most / 127.f / sqrtf(s.ss / (float)k + a.eps);
             } else {
                 // rows of zeros, of values whose squares or quotients leave fp32, or with a NaN: the row's largest value is brought to 1..2
                 RowStat m = {0.f, 0u};
@@ -178,32 +187,28 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void rows_i8_kernel(cons
                         m.most = b > m.most ? b : m.most;
                     }
                 m = reduce(m);
-                q.ok = m.most < 0x7f800000u;
-                const int e = q.ok && m.most ? -ilogbf(__uint_as_float(m.most)) : 0;
+                const bool ok = m.most < 0x7f800000u;
+                const int e = ok && m.most ? -ilogbf(__uint_as_float(m.most)) : 0;
                 const float p0 = pow2(e / 2), p1 = pow2(e - e / 2);
 #pragma unroll
                 for (int c = 0; c < C; ++c)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) h[c][j] = h[c][j] * p0 * p1;
                 s = stat();
-                q.ok = q.ok && s.most < 0x7f800000u;
-                const float top = __uint_as_float(s.most);
                 const double d0 = p0, d1 = p1;
-                q.scale = q.ok ? (float)((double)top / 127.0 / sqrt((double)s.ss / k + (double)a.eps * d0 * d0 * d1 * d1)) : __uint_as_float(0x7fc00000u);
-                q.inv = q.ok && top > 0.f ? 127.f / top : 0.f;
-                q.p0 = q.p1 = 1.f;
+                scale = ok && s.most < 0x7f800000u ? (float)((double)__uint_as_float(s.most) / 127.0 / sqrt((double)s.ss / k + (double)a.eps * d0 * d0 * d1 * d1)) : __uint_as_float(0x7fc00000u);
             }
         }
+        const RowScale q = row_scale(s.most);
         int8_t* codes = a.codes + (size_t)row * a.pitch;
         gain([&](int c, const float* gc) {
             if (at[c] >= a.pitch) return;
-            uint32_t v[8];
+            float v[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = row_code(q, NORM ? h[c][j] * gc[j] : h[c][j]);
-            const u32x2_t o = {v[0] | v[1] << 8 | v[2] << 16 | v[3] << 24, v[4] | v[5] << 8 | v[6] << 16 | v[7] << 24};
-            *reinterpret_cast<u32x2_t*>(codes + at[c]) = o;
+            for (int j = 0; j < 8; ++j) v[j] = NORM ? h[c][j] * gc[j] : h[c][j];
+            *reinterpret_cast<u32x2_t*>(codes + at[c]) = u32x2_t{row_codes4(q, v), row_codes4(q, v + 4)};
         });
-        if (lane == 0 && (WPR == 1 || wv == 0)) a.scales[row] = q.scale;
+        if (lane == 0 && (WPR == 1 || wv == 0)) a.scales[row] = scale;
     }
 }
 

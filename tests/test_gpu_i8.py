@@ -141,6 +141,47 @@ def test_rows_behind_the_last_stay():
     assert torch.equal(codes[:9], want[0]) and torch.equal(scales[:9], want[1])
 
 
+def nearest_codes(x, k):
+    """127 y / max to the nearest whole number, ties to even.  The quotient in 64 bits is exact at ties (254 y = (2 m + 1) max), and all
+    others lie at least 2^-34 from one: with mantissas Y and M of up to 24 bits and quotients of 1/2 and more, |254 Y / 2^a - (2 m + 1) M| / 2 M
+    with a whole Y 2^-a down to 2^-8."""
+    y = x.double()
+    most = y.abs().amax(1, keepdim=True)
+    return torch.round(127 * y / torch.where(most > 0, most, torch.ones_like(most)))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("k", [8, 1000, 5000, 20000])
+def test_codes_between_two_whole_numbers_go_to_the_even_one(k, dtype):
+    """Half of a row's largest value lies between 63 and 64, whatever that value is: 64, for the codes of rows, the norm's with gain 1,
+    and a layer's channels alike; and of bf16 rows every code is the nearest."""
+    import paper_2102_08481_amd as thia
+    m = torch.arange(128, 256, device="cuda").float()
+    most = torch.cat([m * 2.0 ** e for e in (-118, -107, -60, -8, 0, 50, 93, 119)])
+    x = (rows_of(k, len(most), k, F).clamp(-8, 8) / 8 * most[:, None]).to(dtype)
+    x[:, 0], x[:, 3], x[:, 5] = most.to(dtype), (most / 2).to(dtype), (-most / 2).to(dtype)
+    assert torch.equal(x[:, 3].double() * 2, most.double())
+    q = thia.thia_quantize_rows(x)[0][:, :k].double()
+    assert (q[:, 0] == 127).all() and (q[:, 3] == 64).all() and (q[:, 5] == -64).all()
+    one = torch.ones(k, device="cuda")
+    n = thia.thia_rms_norm_i8(x, one, 1e-6)[0][:, :k].double()
+    assert torch.equal(n, q)
+    want = nearest_codes(x, k)
+    if dtype is BF:
+        assert torch.equal(q, want)
+    else:   # (the quotient is held in fp32: half a step of 2^-17 where it is largest)
+        t = 127 * x.double() / most.double()[:, None]
+        assert ((q - t).abs() <= 0.5 + 2.0 ** -18).all()
+    # a layer's channels: seen through rows that have one code each
+    codes = torch.eye(8, 128, device="cuda").to(torch.int8)
+    fine = most < 2.0 ** 100   # (codes * scale of the others leave fp32)
+    w = x[fine][:, :8].float().contiguous()
+    layer = thia.thia_linear_i8_load(w)
+    s = thia.thia_quantize_rows(w)[1]
+    out = thia.thia_linear_i8_run(layer, codes, torch.ones(8, device="cuda"), out_f32=True)
+    assert torch.equal(out, q[fine][:, :8].t().float().contiguous() * s)
+
+
 # ---------------------------------------------------------------- the product
 def layer_of(seed, n, k, low=-127):
     import paper_2102_08481_amd as thia
