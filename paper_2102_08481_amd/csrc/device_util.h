@@ -121,6 +121,7 @@ __device__ inline bool iou_over(const Box& a, const Box& b, float thr) {
 // ---- rows in 8 bits: scale and codes of a row from the bits of its largest size (infinity and NaN sort last)
 __device__ inline uint32_t size_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 __device__ inline float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+__device__ inline double pow2_64(int e) { return __longlong_as_double((long long)(e + 1023) << 52); }
 // Codes are the quotient 127 v / top in fp32, rounded to nearest even.  127 / top is held as two numbers, inv + rest: with one alone half of the
 // largest value (and whatever else lies on the border of two codes) fell to either side of it.  With two the quotient is the true one rounded
 // once, so a border stays one, and of bf16 rows every code is the nearest: a quotient between 2^(n-1) and 2^n that is no border lies more than
@@ -133,17 +134,17 @@ __device__ inline RowScale row_scale(uint32_t most) {
     if (most && r.ok) {
         const float top = __uint_as_float(most);
         r.inv = 127.f / top;
-        r.rest = __builtin_fmaf(-r.inv, top, 127.f) * (r.inv / 127.f);   // (the first factor exact)
+        r.rest = __builtin_fmaf(-r.inv, top, 127.f) * (r.inv * (1.f / 127.f));   // (the first factor exact)
     }
     return r;
 }
-// Codes of four values in the bytes of a word.  Behind the addition a number's lowest bits are the nearest whole number to it.
+// Behind the addition a number's lowest bits are the nearest whole number to it, and its last byte the code.
+__device__ inline uint32_t row_code(const RowScale& r, float v) { return __float_as_uint(__builtin_fmaf(v, r.inv, v * r.rest) + 12582912.f); }
+// Codes of four values in the bytes of a word.
 __device__ inline uint32_t row_codes4(const RowScale& r, const float* v) {
     if (!r.ok) return 0u;
-    uint32_t c[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) c[j] = __float_as_uint(__builtin_fmaf(v[j], r.inv, v[j] * r.rest) + 12582912.f);
-    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[3], c[2], 0x0c0c0400u), __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400u), 0x05040100u);
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(row_code(r, v[3]), row_code(r, v[2]), 0x0c0c0400u),
+                                 __builtin_amdgcn_perm(row_code(r, v[1]), row_code(r, v[0]), 0x0c0c0400u), 0x05040100u);
 }
 // Of rows as they are: the scale (NaN if the row is not finite) and the power of two that brings rows outside 1e-30 to 1e30 back into it, 1 for all others.
 __device__ inline float row_step(uint32_t most, float& power) {

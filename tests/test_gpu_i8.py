@@ -108,6 +108,59 @@ def test_norm_with_zero_and_large_gains():
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("k", [5, 300, 2000, 9000, 40000])
+def test_norm_with_gains_at_the_ends_of_fp32(k, dtype):
+    """y is finite and its codes reach 127 whatever the gain's size: products of a value and a gain that leave fp32 on either side, also
+    where the row's largest values have no gain.  The eps lies far below, near and far above the mean of the squares."""
+    import paper_2102_08481_amd as thia
+    x = rows_of(k + 3, 6, k, dtype)
+    x[4] *= 2.0 ** -60
+    x[5] *= 2.0 ** 60
+    sign = torch.where(rows_of(1, 1, k, F)[0] > 0, 1.0, -1.0)
+    for size in (1e-36, 1e-37, 1e-38, 2.0 ** -130, 2.0 ** -149, 1e38, 3.4e38):
+        gain = sign * size
+        for eps in (1e-38, 1.0, 1e38):
+            codes, scales, _ = thia.thia_rms_norm_i8(x, gain, eps)
+            h = x.double()
+            check_codes(codes, scales, h * gain.double() / torch.sqrt((h * h).mean(1, keepdim=True) + eps), k, 64)
+            assert (codes.abs().amax(1) == 127).all()
+    some = torch.arange(k, device="cuda") % 4 == 0
+    x[:, some] = x[:, some].sign() * 2.0 ** 126
+    for size in (2.0 ** -100, 1.0, 3e38):   # (y's largest is 2^-186 or so times the gain: the codes hold where the scale no longer does)
+        gain = torch.where(some, 0.0, size)
+        codes, scales, _ = thia.thia_rms_norm_i8(x, gain, 1e-6)
+        h = x.double()
+        check_codes(codes, scales, h * gain.double() / torch.sqrt((h * h).mean(1, keepdim=True) + 1e-6), k, 64)
+        assert (codes.abs().amax(1) == 127).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("k", [37, 3000, 20000])
+def test_norm_of_unusual_rows_in_place(k, dtype):
+    """Rows whose products or squares leave fp32, rows of zeros and rows that are no numbers between ordinary ones, the sum in place of
+    either input or beside them."""
+    import paper_2102_08481_amd as thia
+    x, r = rows_of(k, 23, k, dtype), rows_of(k + 1, 23, k, dtype)
+    for i, size in ((3, 2.0 ** -70), (4, 2.0 ** 70), (9, 0.0), (10, 2.0 ** -120), (16, 2.0 ** 120)):
+        x[i] *= size
+        r[i] *= size
+    x[7, k // 2], r[12, 0] = float("inf"), float("nan")
+    fine = torch.tensor([i for i in range(23) if i not in (7, 12)], device="cuda")
+    for size in (1.0, 1e-37, 1e37):
+        gain = (0.5 + torch.rand(k, device="cuda")) * size
+        codes, scales, total = thia.thia_rms_norm_i8(x, gain, 1e-6, r)
+        assert torch.equal(total[fine], (x.float() + r.float()).to(dtype)[fine]) and total[7, k // 2].isinf() and total[12, 0].isnan()
+        h = (x.float() + r.float()).double()[fine]
+        check_codes(codes[fine], scales[fine], h * gain.double() / torch.sqrt((h * h).mean(1, keepdim=True) + 1e-6), k, 64)
+        assert scales[7].isnan() and scales[12].isnan() and (codes[7] == 0).all() and (codes[12] == 0).all()
+        for target in (0, 1):
+            y = [x.clone(), r.clone()]
+            got = thia.thia_rms_norm_i8(y[0], gain, 1e-6, y[1], sum_out=y[target])
+            assert torch.equal(got[0], codes) and torch.equal(got[1][fine], scales[fine]) and torch.equal(got[2][fine], total[fine])
+            assert torch.equal(y[1 - target].isnan(), (x, r)[1 - target].isnan())
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("k", [37, 1000, 4099])
 def test_rows_with_pitches_on_odd_addresses_and_sums_in_place(k, dtype):
     import paper_2102_08481_amd as thia
