@@ -114,7 +114,8 @@ int thia_set_lanes(thia_model* m, int lanes);
  * layer's results become 8-bit codes (thia_quantize_rows) and meet weights quantized per channel (thia_linear_i8_run), every
  * exit's; the layers' results keep the model's type and the predictors their own arithmetic.  An approximation of the model's
  * head; frames stay independent of each other.  Blocking: the weights are quantized, or freed, by the call, and the
- * next call enlarges the workspace.  THIA_E_SHAPE if a region has more than 65536 features. */
+ * next call enlarges the workspace.  The model's device must be the current one.  THIA_E_SHAPE if a region has more than 65536
+ * features. */
 int thia_set_head_bits(thia_model* m, int bits);
 
 int thia_get_info(const thia_model* m, thia_info* out);

@@ -1219,6 +1219,13 @@ int thia_set_lanes(thia_model* m, int lanes) {
 int thia_set_head_bits(thia_model* m, int bits) {
     if (!m) return THIA_E_BADARG;
     if (bits != 0 && bits != 8) return fail(m, THIA_E_BADARG, "head bits must be 0 (the model's own type) or 8");
+    if (bits == 8) {   // the layers are made on the current device, and products refuse any other than their own
+        int dev = 0;
+        hipPointerAttribute_t at;
+        HIP_TRY(m, hipGetDevice(&dev));
+        HIP_TRY(m, hipPointerGetAttributes(&at, m->ex[0].fc1.w));
+        if (at.device != dev) return fail(m, THIA_E_BADARG, "the model lies on another device than the current one");
+    }
     HIP_TRY(m, hipStreamSynchronize(m->stream));
     if (m->lane_stream) HIP_TRY(m, hipStreamSynchronize(m->lane_stream));
     int rc = THIA_OK;

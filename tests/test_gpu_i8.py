@@ -597,3 +597,17 @@ def test_box_head_in_8_bits(precision, head_ch):
         model.set_head_bits(0)
     assert all(torch.equal(a, b) for a, b in zip(before, model.detect_chunk(frames, ep)))
     assert not torch.equal(before[1], eight[1])   # the option does something
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two devices")
+def test_head_bits_belong_to_the_models_device():
+    """The 8-bit layers are refused while another device is current, and the model stays as it was."""
+    import numpy as np
+    import paper_2102_08481_amd as thia
+    from gpu_common import MINI_BF16, biased_model
+    model, _ = biased_model(MINI_BF16, 77)
+    frames = torch.from_numpy(np.random.RandomState(5).randint(0, 256, (1, 3, 130, 190)).astype(np.uint8)).cuda()
+    before = [v.clone() for v in model.detect_chunk(frames, 1)]
+    with torch.cuda.device(1), pytest.raises(thia.ThiaError):
+        model.set_head_bits(8)
+    assert all(torch.equal(a, b) for a, b in zip(before, model.detect_chunk(frames, 1)))
