@@ -315,6 +315,46 @@ def test_linear_ragged(rows, k, n, dtype):
     assert torch.equal(inplace, want)
 
 
+# ragged too, with channels in eights: every tile by accesses of 16 bytes, and by single elements where the pitch is odd
+RAGGED_WIDE = [(5, 200, 40), (701, 640, 136), (1003, 390, 520), (2001, 1000, 1000), (1187, 12001, 1000), (2003, 12544, 1000), (3365, 260, 1080), (2001, 200, 1992),
+               (9001, 130, 1000), (2901, 300, 2008), (4001, 300, 4008), (4097, 700, 4104)]
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("rows,k,n", RAGGED_WIDE)
+def test_linear_ragged_by_16_bytes(rows, k, n, dtype):
+    """Rows and channels that end inside the tile where rows take 16-byte accesses: dense and pitched, in place, the same bits as element by
+    element, nothing written beside them."""
+    import paper_2102_08481_amd as thia
+    layer, w, ws, b = layer_of(rows + n, n, k)
+    codes, scales = codes_of(k, rows, k)
+
+    def pitched(columns, first):
+        return torch.full((rows + 2, n + columns), 7, dtype=dtype, device="cuda")[:rows, first:first + n]
+
+    def run(relu, res, out=None):
+        return thia.thia_linear_i8_run(layer, codes, scales, relu, res, dtype is F, out)
+
+    res = rows_of(9, rows, n, dtype) * 100
+    for relu, residual in ((True, None), (False, res), (True, res)):
+        want = run(relu, residual)
+        check_product(want, codes, scales, w, ws, b, k, relu, residual)
+        for columns, first in ((16, 8), (7, 3)):   # (the second: element by element)
+            r = residual
+            if r is not None:
+                r = pitched(columns, first)
+                r.copy_(residual)
+            out = pitched(columns, first)
+            room = out._base
+            assert run(relu, r, out).data_ptr() == out.data_ptr() and torch.equal(out, want)
+            out.fill_(7)
+            assert (room == 7).all()
+            if r is not None:
+                assert torch.equal(run(relu, r, r), want)
+                r.fill_(7)
+                assert (r._base == 7).all()
+
+
 def test_more_rows_than_one_launch_holds():
     import paper_2102_08481_amd as thia
     layer, w, ws, b = layer_of(3, 3, 5)
