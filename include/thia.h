@@ -113,9 +113,9 @@ int thia_set_lanes(thia_model* m, int lanes);
 /* Type of the box head's two wide layers: bits = 0 (the default): the model's own; 8: rows of region features and of the first
  * layer's results become 8-bit codes (thia_quantize_rows) and meet weights quantized per channel (thia_linear_i8_run), every
  * exit's; the layers' results keep the model's type and the predictors their own arithmetic.  An approximation of the model's
- * head; frames stay independent of each other.  Blocking: the weights are quantized, or freed, by the call, and the
- * next call enlarges the workspace.  The model's device must be the current one.  THIA_E_SHAPE if a region has more than 65536
- * features. */
+ * head: class logits and box deltas move by 1 to 2 % in the root mean square (random weights), boxes of 540 x 960 frames by about 0.3
+ * pixels; frames stay independent of each other.  Blocking: the weights are quantized, or freed, by the call, and the next call
+ * enlarges the workspace.  The model's device must be the current one.  THIA_E_SHAPE if a region has more than 65536 features. */
 int thia_set_head_bits(thia_model* m, int bits);
 
 int thia_get_info(const thia_model* m, thia_info* out);
@@ -504,7 +504,7 @@ typedef struct thia_linear_i8 thia_linear_i8;
 int thia_linear_i8_load(const float* weights, const float* bias, int n, int k, thia_linear_i8** out);
 int thia_linear_i8_load_codes(const int8_t* codes, const float* scales, const float* bias, int n, int k,
                               thia_linear_i8** out);
-/* Frees the weights; waits for the device.  NULL is allowed. */
+/* Frees the weights; waits for the device (so not while a stream is captured).  NULL is allowed. */
 void thia_linear_i8_free(thia_linear_i8* l);
 int thia_linear_i8_shape(const thia_linear_i8* l, int* n, int* k);
 

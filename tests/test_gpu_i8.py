@@ -639,6 +639,49 @@ def test_box_head_in_8_bits(precision, head_ch):
     assert not torch.equal(before[1], eight[1])   # the option does something
 
 
+@pytest.mark.parametrize("precision", [1, 0])
+def test_how_far_the_head_in_8_bits_is_from_the_models_own(precision):
+    """Logits and deltas of the two heads on the same region features.  A code is off by at most half a step of its row, step / sqrt(12) in the
+    mean square if what is rounded off is spread evenly, and those errors are independent of one another: their squares add up along the
+    products, through both layers and the predictors, as do those of the results' rounding to bf16.  They would have to double for errors
+    of half a step each (sqrt(3) of the even spread); twice the predicted deviation holds for each exit's logits and deltas taken together."""
+    import numpy as np
+    from gpu_common import MINI_BF16, MINI_FP32, biased_model
+    from thia_synth import split_blob
+    spec = MINI_BF16 if precision else MINI_FP32
+    model, blob = biased_model(spec, 77)
+    frames = torch.from_numpy(np.random.RandomState(6).randint(0, 256, (2, 3, 130, 190)).astype(np.uint8)).cuda()
+    dtype, rows = BF if precision else F, 2 * spec.post_nms
+    for ep in (1, spec.n_exits):
+        t = {n: torch.from_numpy(v.copy()).cuda() for n, v in split_blob(spec, blob).items() if n.startswith(f"e{ep}.")}
+        w = {n: t[f"e{ep}.{n}.w"].to(dtype).double() for n in ("fc1", "fc2", "cls", "box")}
+        w["fc1"] = w["fc1"].reshape(spec.fc_dim, -1, 49).transpose(1, 2).reshape(spec.fc_dim, -1)
+        taps = {}
+        try:
+            model.set_debug(True)
+            for bits in (0, 8):
+                model.set_head_bits(bits)
+                model.detect_chunk(frames, ep)
+                torch.cuda.synchronize()
+                taps[bits] = {n: torch.from_numpy(model.tap(n).copy()).cuda().double().reshape(rows, -1) for n in ("roi_feat", "cls_logits", "box_deltas")}
+        finally:
+            model.set_debug(False)
+            model.set_head_bits(0)
+        assert torch.equal(taps[0]["roi_feat"], taps[8]["roi_feat"])
+        h, var = taps[0]["roi_feat"], 0.0
+        for n in ("fc1", "fc2"):
+            a, b = h.abs().amax(1, keepdim=True) / 127, w[n].abs().amax(1) / 127   # the steps
+            wt = w[n].t().contiguous()
+            var = (var + (h != 0) * a * a / 12) @ (wt * wt) + (h * h) @ ((wt != 0) * b * b / 12)
+            h = (h @ wt + t[f"e{ep}.{n}.b"].double()).clamp(min=0)
+            var = var * (h > 0) + (2 * (h * HALF[dtype]) ** 2 / 3 if precision else 0)
+        for name, n in (("cls_logits", "cls"), ("box_deltas", "box")):
+            wt = w[n].t().contiguous()
+            off = taps[8][name] - taps[0][name]
+            got, predicted = (off * off).mean().sqrt(), (var @ (wt * wt)).mean().sqrt()
+            assert 0 < got <= 2 * predicted
+
+
 @pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two devices")
 def test_head_bits_belong_to_the_models_device():
     """The 8-bit layers are refused while another device is current, and the model stays as it was."""
