@@ -484,14 +484,15 @@ const char* thia_i8_last_error(void);
 /* Bytes from one row of codes to the next; 0 if k is not within 1..65536. */
 int thia_i8_pitch(int k);
 
-/* Rows x dev T [rows, k] (pitch ldx) -> codes, scales dev float32 [rows]. */
+/* Rows x dev T [rows, k] (pitch ldx) -> codes, scales dev float32 [rows]; neither may overlap x. */
 int thia_quantize_rows(const void* x, long long ldx, int precision, int rows, int k, int8_t* codes, float* scales,
                        void* hip_stream);
 
 /* The residual's addition and a root-mean-square norm in front of an 8-bit product, in one pass: h = x + residual in fp32,
  * sum = h rounded to T, y[j] = h[j] gain[j] / sqrt(mean(h^2) + eps), y's codes and scales as above.  x, residual (NULL: h = x) and
  * sum (NULL: not wanted; needs a residual) dev T [rows, k] with pitches ldx, ldr, ldsum; sum may be x or residual itself (same pitch), and
- * must not overlap them otherwise.  gain dev float32 [k].  eps > 0. */
+ * must not overlap them otherwise; codes and scales overlap nothing.  gain dev float32 [k], any finite values: y's direction is formed in
+ * fp32, where its products leave that range in 64 bits (such rows take several times as long).  eps > 0. */
 int thia_rms_norm_i8(const void* x, long long ldx, const void* residual, long long ldr, const float* gain, float eps,
                      int precision, int rows, int k, void* sum, long long ldsum, int8_t* codes, float* scales,
                      void* hip_stream);
@@ -509,7 +510,7 @@ void thia_linear_i8_free(thia_linear_i8* l);
 int thia_linear_i8_shape(const thia_linear_i8* l, int* n, int* k);
 
 /* out[m, c] = act(scales[m] wscale[c] sum_j codes[m, j] wcodes[c, j] + bias[c] + residual[m, c]): the sum exact in 32-bit whole
- * numbers, the rest in fp32, one rounding to T.  codes, scales as above ([rows, thia_i8_pitch(k)], [rows]; -128 is allowed), residual
+ * numbers, the rest in fp32 (the sum times scales[m] first, which has to stay in its range), one rounding to T.  codes, scales as above ([rows, thia_i8_pitch(k)], [rows]; -128 is allowed), residual
  * dev T [rows, n] (pitch ldr) or NULL, relu 0 or 1 (a NaN stays), out dev T [rows, n] (pitch ldo), T per precision.  out may be
  * residual itself (same pitch) and must not overlap any input otherwise.  A row's result does not depend on the other rows or on
  * their number.  The layer's device must be the current one. */

@@ -202,6 +202,8 @@ __device__ inline void finish_rows(const LinearArgs& a, const i32x16_t (&acc)[2]
                 store8(static_cast<T*>(a.out) + (m0 + rj + r) * a.ldo + nw + c, o);
             }
         } else if (nw + lane < a.n) {
+            // (element by element; out may be the residual, so each row's residual is waited for behind the store in front of it: 4001 x 1024 x 4099
+            // 41 us, with a residual 85; x 4104 31 and 37)
             for (int r = 0; r < 32 && rj + r < rows; ++r) {
                 const size_t m = m0 + rj + r;
                 float o[1] = {*reinterpret_cast<const float*>(ep + (size_t)r * FINISH_PITCH + lane * 4)};

@@ -15,10 +15,11 @@
 // memory part.  A half that phase j reads has landed for all wavefronts when phase j starts: each waits in phase j - 1, in front of its
 // barrier, until no more of its requests are outstanding than it issued behind that half (vmcnt counts them in order).
 //
-// 8192 x 8192 x 8192 takes 423 us (2.6 POP/s; a library's product of 8-bit integers without scales 524), 9600 x 12544 x 1024 on 200 blocks of
-// 192 x 256 107 us (2.3 POP/s; 197).  The matrix pipes are busy in 74 % of the cycles there, and the chip's clock comes down to 1.4 GHz under them:
-// a K tile of 256 x 256 takes 0.96 us while a few CUs work and 1.6 when all do.  About 8 us per block do not grow with K (launch,
-// first operands, results, which all blocks of a round write at once: 4096 x 1024 x 4096 takes 22 us for 14 us of products).
+// 8192 x 8192 x 8192 takes 436 to 444 us (2.5 POP/s), with a residual 458 to 461, on a card where a library's product of 8-bit integers without
+// scales takes 455 on the same codes, and up to 512 on others; 9600 x 12544 x 1024 on 200 blocks of 192 x 256 106 to 111 us (2.3 POP/s; 197).
+// The matrix pipes are busy in 74 % of the first one's cycles and in 56 % of the second's, whose blocks leave 56 CUs free, and the chip's clock comes
+// down to 1.4 GHz under them: a K tile of 256 x 256 takes 0.96 us while a few CUs work and 1.6 when all do.  About 8 us per block do not grow
+// with K (launch, first operands, results, which all blocks of a round write at once: 4096 x 1024 x 4096 takes 24 us for 14 us of products).
 //
 // Part of linear_i8.h, which includes it once.
 template <typename T, int BM>

@@ -3,7 +3,7 @@
 // Fragments of the next K tile are read between the products of this one.
 //
 // A K tile of a 128 x 128 block is 512 cycles of products per SIMD, 64 KB of fragment reads and 32 KB of requests (768 cycles of LDS).
-// 4096 x 4096 x 1024 (256 blocks) takes 23.3 us; without its requests it was 21, without fragment reads as well 19.5, of which about 5
+// 4096 x 4096 x 1024 (256 blocks) takes 23 to 25 us by card; where it was 23.3, without its requests it was 21, without fragment reads as well 19.5, of which about 5
 // are launch, first operands and results: products at the clock that the chip keeps under matrix work are most of it.  Requests
 // issued together in front of the products held up everything behind them (900 x 12544 x 1024 52 us, between the products 46).
 //

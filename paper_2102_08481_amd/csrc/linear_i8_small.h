@@ -2,11 +2,12 @@
 // pieces w, w + W, ... of every row, with D pieces on their way while one is multiplied, and waits for no other wavefront.
 // The W partial sums meet in LDS (whole numbers: their order does not matter).
 //
-// What bounds it is how fast a CU can fetch its operands: 300 x 12544 x 1024 on 160 tiles of 32 x 64 takes 15.5 us with the products and
+// What bounds it is how fast a CU can fetch its operands: 300 x 12544 x 1024 on 160 tiles of 32 x 64 takes 15.0 to 15.5 us with the products and
 // without them, 8.8 with the weights alone and 7.1 with the rows alone; a block fetches 1.2 MB in it, 95 KB per us (hits in L2 come
 // at 117 to 141 KB per us and CU, whatever the pattern).  More pieces on their way or more wavefronts change nothing (D 2: 15.6, 8
 // wavefronts: 15.3); fragments straight from memory, 32 rows of 32 bytes a request, took 20 us.  So the tile's shape is what
-// counts: more CUs at work against fewer bytes per product.
+// counts: more CUs at work against fewer bytes per product.  128 x 64 tiles take all of a wavefront's registers (388) and spill 8 bytes,
+// outside the loop.
 //
 // Part of linear_i8.h, which includes it once.
 //

@@ -7,18 +7,19 @@ namespace thia {
 // Which tile: the one with the least base + K tiles * (per_k * rounds + more_k * (r - 1)) + per_tile * r, in us, where r is the number of tiles
 // per CU, at least 1, and `rounds` that number rounded up.  The constants are a least-squares fit (relative errors) to what the tiles took on
 // 240 shapes of 1 to 16 384 rows, 128 to 12 544 columns and 64 to 8 192 channels; over these the rule is 1.4 % from the best tile in the geometric
-// mean, and 29 % at worst.  Measured in us, rows x columns x channels:
+// mean, and 29 % at worst.  Measured in us (bf16 results, back to back in a captured graph), rows x columns x channels:
 //                        16x16  32x32  32x64  64x64  96x64  128x64  128x128  192x256  256x256
-//   1 x 4096 x 4096        3.7    4.6    5.4    6.9
-//   130 x 4096 x 512       7.4    4.8    5.8    7.5
-//   700 x 256 x 2048       9.9    6.5    4.9    5.5    5.8     6.9      7.1      8.6
-//   700 x 12544 x 1024             34     29     21     26      30
-//   1200 x 12544 x 1024            69     46     39     27      32       45
-//   2000 x 12544 x 1024           112     64     59     57      38       46
-//   4000 x 1024 x 1024             21     14     14     17      16       11       14       16
-//   9600 x 1024 x 1024                    31     31     42      44       27       17       19
-//   4000 x 4096 x 4096                                                   98       78       60
-//   9600 x 12544 x 1024                                                 158      107      120
+//   1 x 4096 x 4096        3.3    4.3    5.1    6.6
+//   130 x 4096 x 512       7.1    4.4    5.3    7.2
+//   700 x 256 x 2048       9.4    6.0    4.4    5.0    5.3     6.5      6.8      8.4
+//   700 x 12544 x 1024             34     28     21     25      30
+//   1200 x 12544 x 1024            69     45     39     27      31       45
+//   2000 x 12544 x 1024           112     63     60     57      39       46
+//   4000 x 1024 x 1024             21     14     13     16      16       10       13       16
+//   9600 x 1024 x 1024                    32     31     42      43       27       17       18
+//   4000 x 4096 x 4096                                                   97       78       60
+//   9600 x 12544 x 1024                                                 159      106      114
+// It does not know whether rows take 16-byte accesses: with odd channels and a residual the epilogue of the larger tiles outweighs the rest (see finish_rows).
 struct Tile { int rows, chans; double base, per_k, per_tile, more_k; };
 constexpr Tile kTiles[] = {{16, 16, 2.67, 0.065, 0.120, 0.038},  {32, 32, 2.61, 0.060, 0.515, 0.018},   {32, 64, 2.77, 0.088, 0.513, 0.042},
                            {64, 64, 2.61, 0.139, 1.366, 0.061},  {96, 64, 0.58, 0.224, 4.041, 0.0},     {128, 64, 1.53, 0.271, 4.688, 0.056},

@@ -1,8 +1,9 @@
 // Single rows and the smallest products: 16 rows x 16 channels per block of W wavefronts that share the contraction as in linear_i8_small.h.
 // What bounds these is how fast a CU can fetch (about 100 KB per us), so the smallest tile, which gives the most CUs a share,
-// is the fastest although it fetches the most: one row x 12544 x 1024 5.5 us (32 x 32 tiles 8.2), x 4096 x 4096 3.9 (4.7; 16.8 MB from the
-// caches), x 8192 x 128 4.5 (6.2).  More wavefronts per block lose (8: 5.8, 4.2 and 4.7).  Both operands come straight from memory, lane l taking row l % 16 and the 16-byte
-// chunk l / 16 of 64 k: 64 bytes of each of 16 rows, of the weights four runs of 256 bytes.
+// is the fastest although it fetches the most: one row x 12544 x 1024 5.1 us (32 x 32 tiles 7.8), x 4096 x 4096 3.3 (4.3; 16.8 MB from the
+// caches), x 8192 x 128 4.1 (5.8), back to back in a captured graph.  More wavefronts per block lose (8: 0.2 to 0.3 us more).  Both operands come
+// straight from memory, lane l taking row l % 16 and the 16-byte chunk l / 16 of 64 k: 64 bytes of each of 16 rows, of the weights four runs
+// of 256 bytes.
 //
 // Part of linear_i8.h, which includes it once.
 template <typename T, int W>

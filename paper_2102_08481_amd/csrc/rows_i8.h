@@ -82,8 +82,8 @@ struct RowArgs {
     int rows, k, pitch;
 };
 
-// Up to so many pieces of eight per lane the gain stays in registers from row to row; beyond, its registers cost more than its
-// reads from the caches (us, held / read: 9 600 x 1 024 12.8 / 13.9, 16 384 x 4 096 in two pieces 99 / 119, 4 096 x 16 384 in four 138 / 109).
+// Up to so many pieces of eight per lane the gain stays in registers from row to row (us, held / read: 9 600 x 1 024 12.8 / 14.9, 16 384 x 4 096 in two
+// pieces 97 / 124).  More pieces are taken by rows of sixteen wavefronts alone, of whose 128 registers four pieces leave 23.
 constexpr int kHold = 2;
 // A row per WPR wavefronts, 8 C values of it per lane, in registers from the one load to the codes' store; with WPR 1 four rows
 // per block.  Blocks walk over the rows, so that the gain stays in registers.  (Eight wavefronts per SIMD with few values per lane: 64 registers, so
@@ -283,16 +283,16 @@ template <typename T, bool NORM, int WPR, int C>
 hipError_t launch_cfg(const RowArgs& a, hipStream_t s) {
     constexpr int RPB = WPR == 1 ? 4 : 1, THREADS = WPR == 1 ? 256 : WPR * 64;
     // Blocks that the chip holds at once walk over the rows; without a gain to keep, a wide row is a block of its own, so that a last
-    // round is not waited for (us, walking / a block per row: norm of 8 192 x 8 192 91 / 105, codes of 9 600 x 12 544 89 / 74).
+    // round is not waited for (us, walking / a block per row: norm of 8 192 x 8 192 85 / 86, codes of 9 600 x 12 544 84 / 70).
     const long long groups = ((long long)a.rows + RPB - 1) / RPB, most = !NORM && WPR > 1 ? 1 << 21 : 256ll * 2048 / THREADS;
     hipLaunchKernelGGL((rows_i8_kernel<T, NORM, WPR, C>), dim3((unsigned)(groups < most ? groups : most)), dim3(THREADS), 0, s, a);
     return hipGetLastError();
 }
 
-// Up to 1024 values a wavefront per row, which needs no barrier (9 600 x 1 024 norm in us: one wavefront 13.1, two 13.5, four
-// 16.3).  Beyond, a row is spread until a lane has eight values of it for the norm, which holds most registers (us, 8 / 16 / 32 values per
-// lane: 16 384 x 4 096 90 / 98 / 126, 8 192 x 8 192 91 / 96 / 111), and sixteen or 32 without it (8 192 x 8 192 38 / 33 / 35, 16 384 x 4 096 36 / 32 /
-// 34); with few rows the wider spread is the quicker too (one row of 8 192: norm 4.3 / 4.4 / 6.1, codes 3.4 / 3.4 / 3.9).
+// Up to 1024 values a wavefront per row, which needs no barrier (9 600 x 1 024 norm in us: one wavefront 12.8, two 12.5, four
+// 15.3).  Beyond, a row is spread until a lane has eight values of it for the norm, which holds most registers (us, 8 / 16 / 32 values per
+// lane: 16 384 x 4 096 88 / 97 / 127, 8 192 x 8 192 85 / 96 / 110), and sixteen or 32 without it (8 192 x 8 192 38 / 31 / 32, 16 384 x 4 096 33 / 30 /
+// 32); with few rows the wider spread is as quick (one row of 8 192: norm 3.4 / 3.4 / 5.3, codes 2.7 / 2.7 / 3.1).
 template <typename T, bool NORM>
 hipError_t launch_rows(const RowArgs& a, hipStream_t s) {
     const int k = a.k;
